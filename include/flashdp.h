@@ -223,6 +223,79 @@ size_t flashdp_workspace_bytes_chunked(const flashdp_layer_t* layers, int n_laye
 /* Number of samples the last block call on this thread parked at a time (B when the batch was not chunked). */
 int64_t flashdp_last_chunk(void);
 
+/* ---- The layers around the weight gradient ------------------------------------------------------------------------
+ *
+ * What else a transformer block has that is trained under per-layer DP-SGD: the forward product with its epilogue, the
+ * backward pass of its activation and the DP gradients of biases and normalisations, and activations kept in 8 bits.  The
+ * conventions above hold (device pointers, 16-byte aligned, rows one after the other, work enqueued on `stream`, argument errors
+ * before anything is enqueued), with these additions:
+ *   - any positive sizes are accepted, d_in, d_out and d up to 2^30, rows (B * T) below 2^40; rows need no alignment of their own;
+ *   - parameters (W, bias, gamma, beta) and activations have the type `dtype`; arithmetic is fp32, results are rounded once;
+ *   - optional pointers may be NULL;
+ *   - a workspace argument works as for flashdp_block_dp_grad: NULL takes the library-owned one, which is not grown
+ *     while `stream` is being captured (FLASHDP_WORKSPACE_TOO_SMALL instead).
+ *
+ * DP gradients of a vector of parameters v (a bias; gamma and beta of a normalisation, which are one vector gamma, beta):
+ *     g_i = sum_t dv_it     n_i = ||g_i||_2     out_grad = sum_i g_i / max(1, n_i / C) + sigma * C * z
+ * as for a weight, with norms of its own (a bias is not clipped together with its layer's weight: a layer of both has the
+ * sensitivity sqrt(C_weight^2 + C_bias^2)).  z[e] is the noise field above with FLASHDP_FIELD_BIAS or FLASHDP_FIELD_NORM as last word of the
+ * Philox counter, so the parameters of one layer may share (seed, layer).  accumulate and add_noise as in
+ * flashdp_block_dp_grad_micro.  Results repeat to the bit.  A sample whose norm is NaN turns out_grad into NaN; one whose
+ * norm overflows fp64's range of squares does too. */
+enum { FLASHDP_FIELD_BIAS = 1, FLASHDP_FIELD_NORM = 2 };
+
+/* relu(0) has slope 0.  GELU is z Phi(z); GELU_TANH is z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. */
+enum { FLASHDP_ACT_NONE = 0, FLASHDP_ACT_RELU = 1, FLASHDP_ACT_GELU = 2, FLASHDP_ACT_GELU_TANH = 3, FLASHDP_ACT_SILU = 4 };
+
+/* Y = act(Z) + residual, Z = X W^T + bias, for X [rows][d_in], W [d_out][d_in], Y and residual [rows][d_out], bias [d_out].
+ * Z, if not NULL, receives what the backward pass of the activation needs: [rows][d_out] in `dtype` (z_8bit = 0), or an 8-bit checkpoint of
+ * flashdp_checkpoint8_bytes(rows, d_out) bytes made from the fp32 sums (z_8bit = 1).  The activation is taken of the fp32 sum,
+ * not of the kept Z.  Y may be residual; it may overlap nothing else.  Rows are independent of each other to the bit only among calls
+ * of the same number of rows (the order of additions goes by the sizes).  No workspace. */
+int flashdp_linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t rows, int64_t d_in, int64_t d_out,
+                           int dtype, int activation, void* Y, void* Z, int z_8bit, void* stream);
+
+/* The backward pass of flashdp_linear_forward's epilogue: dZ = dY act'(Z) ([B][T][d_out]) and the bias's DP gradient out_grad
+ * [d_out] from g_i = sum_t dZ_it (before dZ is rounded).  Z as flashdp_linear_forward kept it; not used for FLASHDP_ACT_NONE, where dZ
+ * is dY.  (The residual's gradient is dY.)  dZ may be NULL (not wanted) or dY; out_grad may be NULL (no bias: C, sigma, seed, layer and the workspace
+ * are not used), but not both.  Workspace: flashdp_activation_workspace_bytes. */
+int flashdp_activation_dp_grad(const void* dY, const void* Z, int z_8bit, int64_t B, int64_t T, int64_t d_out, int dtype, int activation,
+                               float C, float sigma, uint64_t seed, uint32_t layer, void* dZ, float* out_grad, float* out_norms,
+                               void* workspace, size_t workspace_bytes, void* stream, int accumulate, int add_noise);
+size_t flashdp_activation_workspace_bytes(int64_t B, int64_t T, int64_t d_out, int dtype);
+
+/* Y = (X - mean) rstd gamma + beta over the d features of each row, rstd = 1 / sqrt(variance + eps), eps > 0.  beta may be NULL
+ * (none); mean and rstd [rows] fp32 may be NULL (inference).  Y may be X. */
+int flashdp_layernorm_forward(const void* X, const void* gamma, const void* beta, int64_t rows, int64_t d, int dtype, float eps, void* Y,
+                              float* mean, float* rstd, void* stream);
+
+/* Its backward pass: dX [B][T][d], and the DP gradient of gamma (and beta, with bias != 0) as one vector, out_grad [2][d]
+ * (gamma first) or [d].  dX may be NULL (not wanted) or dY; out_grad may be NULL (frozen parameters), but not both.  Workspace:
+ * flashdp_layernorm_workspace_bytes. */
+int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, const float* mean, const float* rstd, int64_t B, int64_t T, int64_t d,
+                              int dtype, float C, float sigma, uint64_t seed, uint32_t layer, void* dX, float* out_grad, float* out_norms, int bias,
+                              void* workspace, size_t workspace_bytes, void* stream, int accumulate, int add_noise);
+size_t flashdp_layernorm_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype, int bias);
+
+/* Activations in 8 bits.  Blocks of 32 consecutive features of a row share an exponent e, an element is q 2^e:
+ *     m = largest finite magnitude of the block, e = max(floor(log2 m) - 6, -126; fp16: -24),
+ *     q = round(x 2^-e) to the nearest integer, ties to even, cut to -127 .. 127
+ * - off by at most m / 128, and by less than m / 64 where the cut applies.  q 2^e is exact in all three types: unpacking rounds nothing (as fp16, what
+ * was packed from fp16).  A block depends on its own row only, so per-sample gradients from checkpoints are clipped
+ * for what they are, and the privacy guarantee is that of the gradient that is used.  Elements that are not finite come back as NaN.
+ * Buffer: q of all rows, [rows][d] int8, padded to a multiple of 16 bytes (the padding is not written); then e + 127,
+ * [rows][ceil(d / 32)] uint8. */
+size_t flashdp_checkpoint8_bytes(int64_t rows, int64_t d);   /* 0 on invalid arguments */
+int flashdp_checkpoint8_pack(const void* X, int64_t rows, int64_t d, int dtype, void* packed, void* stream);
+int flashdp_checkpoint8_unpack(const void* packed, int64_t rows, int64_t d, int dtype, void* X, void* stream);
+
+/* flashdp_block_dp_grad_micro with every layer's X an 8-bit checkpoint of its [B * T][d_in] activation: each is unpacked to `dtype`
+ * into the workspace (layers in a row with the same X once) and contracted from there, so the memory of one layer's activation is
+ * needed at a time instead of all layers'.  Same schedules and results as unpacking by hand.  Workspace: flashdp_workspace_bytes_checkpoint8. */
+int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule, void* workspace,
+                                      size_t workspace_bytes, void* stream, int accumulate, int add_noise);
+size_t flashdp_workspace_bytes_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule);
+
 /* Non-private weight gradient out_grad = sum_i dY_i^T X_i (Appendix B.1, Eq. "batched-grad") computed by
  * the same contraction kernel with the norm, clip and noise steps switched off: the comparator the DP
  * path is timed against, and the C -> infinity, sigma = 0 special case. */

@@ -15,6 +15,9 @@ LIB_PATH = os.path.join(PKG_DIR, "libflashdp.so")
 
 BF16, F32, F16 = 0, 1, 2
 SCHEDULE_AUTO, SCHEDULE_TWOPASS, SCHEDULE_SCRATCH, SCHEDULE_EXPLICIT, SCHEDULE_OVERLAP, SCHEDULE_GHOST, SCHEDULE_FUSED = 0, 1, 2, 3, 4, 5, 6
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+_ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+FIELD_BIAS, FIELD_NORM = 1, 2
 _SCHEDULES = {"auto": 0, "twopass": 1, "scratch": 2, "explicit": 3, "overlap": 4, "ghost": 5, "fused": 6}
 
 OK = 0
@@ -67,6 +70,23 @@ def lib() -> ctypes.CDLL:
         L.flashdp_linear_dp_grad_static.restype = ci
         L.flashdp_static_scratch_bytes.argtypes = []
         L.flashdp_static_scratch_bytes.restype = sz
+        L.flashdp_linear_forward.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, ci, vp, vp, ci, vp]
+        L.flashdp_activation_dp_grad.argtypes = [vp, vp, ci, i64, i64, i64, ci, ci, f32, f32, u64, u32, vp, vp, vp, vp, sz, vp, ci, ci]
+        L.flashdp_layernorm_forward.argtypes = [vp, vp, vp, i64, i64, ci, f32, vp, vp, vp, vp]
+        L.flashdp_layernorm_dp_grad.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, ci, f32, f32, u64, u32, vp, vp, vp, ci, vp, sz, vp, ci, ci]
+        L.flashdp_checkpoint8_pack.argtypes = [vp, i64, i64, ci, vp, vp]
+        L.flashdp_checkpoint8_unpack.argtypes = [vp, i64, i64, ci, vp, vp]
+        L.flashdp_block_dp_grad_checkpoint8.argtypes = [lp, ci, i64, i64, ci, ci, vp, sz, vp, ci, ci]
+        for n in ("flashdp_linear_forward", "flashdp_activation_dp_grad", "flashdp_layernorm_forward", "flashdp_layernorm_dp_grad",
+                  "flashdp_checkpoint8_pack", "flashdp_checkpoint8_unpack", "flashdp_block_dp_grad_checkpoint8"):
+            getattr(L, n).restype = ci
+        L.flashdp_activation_workspace_bytes.argtypes = [i64, i64, i64, ci]
+        L.flashdp_layernorm_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
+        L.flashdp_checkpoint8_bytes.argtypes = [i64, i64]
+        L.flashdp_workspace_bytes_checkpoint8.argtypes = [lp, ci, i64, i64, ci, ci]
+        for n in ("flashdp_activation_workspace_bytes", "flashdp_layernorm_workspace_bytes", "flashdp_checkpoint8_bytes",
+                  "flashdp_workspace_bytes_checkpoint8"):
+            getattr(L, n).restype = sz
         L.flashdp_plain_grad.argtypes = [vp, vp, i64, i64, i64, i64, ci, vp, vp]
         L.flashdp_plain_grad.restype = ci
         L.flashdp_plain_grad_balanced.argtypes = [vp, vp, i64, i64, i64, i64, ci, vp, vp, sz, vp]
@@ -127,6 +147,14 @@ def dtype_code(t) -> int:
 
 def schedule_code(s) -> int:
     return _SCHEDULES[s] if isinstance(s, str) else int(s)
+
+
+def activation_code(a) -> int:
+    if a is None or isinstance(a, str):
+        if a not in _ACTIVATIONS:
+            raise FlashDPError(INVALID_ARGUMENT, f"activation {a!r}")
+        return _ACTIVATIONS[a]
+    return int(a)
 
 
 # ---- thread-local context -------------------------------------------------------------------------
@@ -285,3 +313,138 @@ def flashdp_contraction_timeline(X, dY, B: int, T: int, d_in: int, d_out: int, p
 def flashdp_mfma_probe(pattern: int, iters: int, workgroups: int, sink, stream=None):
     _check(lib().flashdp_mfma_probe(int(pattern), int(iters), int(workgroups), _ptr(sink), _stream_handle(stream)),
            "flashdp_mfma_probe")
+
+
+# ---- the layers around the weight gradient ----------------------------------------------------------
+
+_FLOATS = {}
+
+
+def _float_type(dtype: int):
+    import torch
+    if not _FLOATS:
+        _FLOATS.update({BF16: torch.bfloat16, F32: torch.float32, F16: torch.float16})
+    return _FLOATS.get(dtype)
+
+
+def _buffer(t, n: int, dtype, where: str) -> Optional[int]:
+    """Address of a tensor that a call uses as a buffer of n elements: rows lie one after the other, and the type is
+    the call's.  (A view with strides of its own, or a shorter one, would be read and written past its end.)"""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < n or not t.is_cuda:
+        raise FlashDPError(INVALID_ARGUMENT, f"{where}: a contiguous device tensor of {dtype} with {n} elements is needed, "
+                                             f"not {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _current(t, where: str):
+    """The library works on the current device; so has the caller's tensor to be."""
+    import torch
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise FlashDPError(INVALID_ARGUMENT, f"{where}: the tensors are on {t.device}, which is not the current device")
+
+
+def _room(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def flashdp_linear_forward(X, W, bias, residual, rows: int, d_in: int, d_out: int, dtype: int, activation, Y, Z=None, z_8bit: bool = False,
+                           stream=None):
+    """Y = act(X W^T + bias) + residual; Z, if given, receives X W^T + bias, in the call's type or as an 8-bit checkpoint (a uint8
+    tensor of flashdp_checkpoint8_bytes(rows, d_out)).  activation: a name or code."""
+    import torch
+    w, f = "flashdp_linear_forward", _float_type(dtype)
+    _current(X, w)
+    z = _buffer(Z, flashdp_checkpoint8_bytes(rows, d_out), torch.uint8, w) if z_8bit else _buffer(Z, rows * d_out, f, w)
+    _check(lib().flashdp_linear_forward(_buffer(X, rows * d_in, f, w), _buffer(W, d_out * d_in, f, w), _buffer(bias, d_out, f, w),
+                                        _buffer(residual, rows * d_out, f, w), rows, d_in, d_out, int(dtype), activation_code(activation),
+                                        _buffer(Y, rows * d_out, f, w), z, int(bool(z_8bit)), _stream_handle(stream)), w)
+
+
+def flashdp_activation_workspace_bytes(B: int, T: int, d_out: int, dtype: int) -> int:
+    return int(lib().flashdp_activation_workspace_bytes(B, T, d_out, int(dtype)))
+
+
+def flashdp_activation_dp_grad(dY, Z, z_8bit: bool, B: int, T: int, d_out: int, dtype: int, activation, C: float, sigma: float, seed: int, layer: int,
+                               dZ, out_grad, out_norms=None, workspace=None, stream=None, accumulate: bool = False, add_noise: bool = True):
+    """dZ = dY act'(Z) and the clipped, noised gradient of the bias (out_grad [d_out] fp32, or None)."""
+    import torch
+    w, f, n = "flashdp_activation_dp_grad", _float_type(dtype), B * T * d_out
+    _current(dY, w)
+    z = _buffer(Z, flashdp_checkpoint8_bytes(B * T, d_out), torch.uint8, w) if z_8bit else _buffer(Z, n, f, w)
+    ws, ws_bytes = _room(workspace)
+    _check(lib().flashdp_activation_dp_grad(_buffer(dY, n, f, w), z, int(bool(z_8bit)), B, T, d_out, int(dtype), activation_code(activation), C, sigma, seed, layer,
+                                            _buffer(dZ, n, f, w), _buffer(out_grad, d_out, torch.float32, w), _buffer(out_norms, B, torch.float32, w),
+                                            ws, ws_bytes, _stream_handle(stream), int(bool(accumulate)), int(bool(add_noise))), w)
+
+
+def flashdp_layernorm_forward(X, gamma, beta, rows: int, d: int, dtype: int, eps: float, Y, mean=None, rstd=None, stream=None):
+    """Y = (X - mean) rstd gamma + beta over rows of d features; mean and rstd [rows] fp32 are kept for the backward pass if given."""
+    import torch
+    w, f = "flashdp_layernorm_forward", _float_type(dtype)
+    _current(X, w)
+    _check(lib().flashdp_layernorm_forward(_buffer(X, rows * d, f, w), _buffer(gamma, d, f, w), _buffer(beta, d, f, w), rows, d, int(dtype), eps,
+                                           _buffer(Y, rows * d, f, w), _buffer(mean, rows, torch.float32, w), _buffer(rstd, rows, torch.float32, w),
+                                           _stream_handle(stream)), w)
+
+
+def flashdp_layernorm_workspace_bytes(B: int, T: int, d: int, dtype: int, bias: bool = True) -> int:
+    return int(lib().flashdp_layernorm_workspace_bytes(B, T, d, int(dtype), int(bool(bias))))
+
+
+def flashdp_layernorm_dp_grad(X, dY, gamma, mean, rstd, B: int, T: int, d: int, dtype: int, C: float, sigma: float, seed: int, layer: int, dX, out_grad,
+                              out_norms=None, bias: bool = True, workspace=None, stream=None, accumulate: bool = False, add_noise: bool = True):
+    """dX and the clipped, noised gradient of gamma and beta (out_grad [2, d] fp32; [d] without a bias; or None)."""
+    import torch
+    w, f, n = "flashdp_layernorm_dp_grad", _float_type(dtype), B * T * d
+    _current(X, w)
+    ws, ws_bytes = _room(workspace)
+    _check(lib().flashdp_layernorm_dp_grad(_buffer(X, n, f, w), _buffer(dY, n, f, w), _buffer(gamma, d, f, w), _buffer(mean, B * T, torch.float32, w),
+                                           _buffer(rstd, B * T, torch.float32, w), B, T, d, int(dtype), C, sigma, seed, layer, _buffer(dX, n, f, w),
+                                           _buffer(out_grad, (2 if bias else 1) * d, torch.float32, w), _buffer(out_norms, B, torch.float32, w), int(bool(bias)),
+                                           ws, ws_bytes, _stream_handle(stream), int(bool(accumulate)), int(bool(add_noise))), w)
+
+
+def flashdp_checkpoint8_bytes(rows: int, d: int) -> int:
+    return int(lib().flashdp_checkpoint8_bytes(rows, d))
+
+
+def flashdp_checkpoint8_pack(X, rows: int, d: int, dtype: int, packed, stream=None):
+    import torch
+    w = "flashdp_checkpoint8_pack"
+    _current(X, w)
+    _check(lib().flashdp_checkpoint8_pack(_buffer(X, rows * d, _float_type(dtype), w), rows, d, int(dtype),
+                                          _buffer(packed, flashdp_checkpoint8_bytes(rows, d), torch.uint8, w), _stream_handle(stream)), w)
+
+
+def flashdp_checkpoint8_unpack(packed, rows: int, d: int, dtype: int, X, stream=None):
+    import torch
+    w = "flashdp_checkpoint8_unpack"
+    _current(packed, w)
+    _check(lib().flashdp_checkpoint8_unpack(_buffer(packed, flashdp_checkpoint8_bytes(rows, d), torch.uint8, w), rows, d, int(dtype),
+                                            _buffer(X, rows * d, _float_type(dtype), w), _stream_handle(stream)), w)
+
+
+def flashdp_workspace_bytes_checkpoint8(layers, B: int, T: int, dtype: int, schedule=SCHEDULE_SCRATCH) -> int:
+    arr = layers if not isinstance(layers, (list, tuple)) else make_layers(layers)
+    return int(lib().flashdp_workspace_bytes_checkpoint8(arr, len(arr), B, T, int(dtype), schedule_code(schedule)))
+
+
+def flashdp_block_dp_grad_checkpoint8(layers, B: int, T: int, dtype: int, schedule=SCHEDULE_AUTO, workspace=None, stream=None,
+                                      accumulate: bool = False, add_noise: bool = True):
+    """flashdp_block_dp_grad_micro with each layer's X an 8-bit checkpoint (a uint8 tensor of flashdp_checkpoint8_bytes(B * T, d_in))."""
+    import torch
+    w = "flashdp_block_dp_grad_checkpoint8"
+    arr = layers
+    if isinstance(layers, (list, tuple)):
+        for L in layers:
+            _current(L["X"], w)
+            _buffer(L["X"], flashdp_checkpoint8_bytes(B * T, L["d_in"]), torch.uint8, w)
+            _buffer(L["dY"], B * T * L["d_out"], _float_type(dtype), w)
+            _buffer(L["out_grad"], L["d_in"] * L["d_out"], torch.float32, w)
+            _buffer(L.get("out_norms"), B, torch.float32, w)
+        arr = make_layers(layers)
+    ws, ws_bytes = _room(workspace)
+    _check(lib().flashdp_block_dp_grad_checkpoint8(arr, len(arr), B, T, int(dtype), schedule_code(schedule), ws, ws_bytes, _stream_handle(stream),
+                                                   int(bool(accumulate)), int(bool(add_noise))), w)

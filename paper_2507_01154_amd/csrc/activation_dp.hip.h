@@ -1,0 +1,118 @@
+// Backward pass of a linear layer's activation and bias: dZ = dY act'(Z) and the bias's per-sample gradient g_i = sum_t dZ_it, as
+// partial sums over chunks of tokens for vector_dp.hip.h.  The bias's sums are taken before dZ is rounded.
+//
+// Memory bound: dY and Z in, dZ out, 6 bytes an element in 16-bit types and 5 with Z in 8 bits.  A thread owns one chunk of 16 bytes of
+// a row and goes down the tokens of its workgroup's chunk, so the sums over tokens stay in registers; the rows of
+// threads join theirs in LDS at the end.  Four rows' loads are in flight per thread.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "activations.hip.h"
+#include "checkpoint8.hip.h"
+#include "vector_io.hip.h"
+
+namespace flashdp {
+
+enum : int { Z_NONE = 0, Z_SAME = 1, Z_EIGHT = 2 };   // how Z is kept
+
+struct ActivationArgs {
+  const void* dY;                 // [B][T][d]
+  const void* Z;                  // [B * T][d], or the q of a checkpoint
+  const unsigned char* scales;    // of a checkpoint
+  void* dZ;                       // may be null, may be dY
+  float* partial;                 // [B][chunks][d]; may be null
+  int64_t B, T, d;
+  int chunks, rows_per_chunk;
+  int col_tiles, log_ct;          // threads side by side: 1 << log_ct, chunks of 16 bytes each
+};
+
+// TOKEN: T == 1, a row is a sample and its gradient dZ itself: the rows of threads take a sample each (and nothing is joined).
+template <int DT, int ACT, int ZK, bool TOKEN>
+__global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs a) {
+  constexpr int N = Chunk<DT>::N, UNROLL = 4;
+  __shared__ float part[TOKEN ? 1 : 256 * N];
+  const int ct = 1 << a.log_ct, rt = 256 >> a.log_ct;
+  const int c = threadIdx.x & (ct - 1), r = threadIdx.x >> a.log_ct;
+  const int64_t unit = blockIdx.x / a.col_tiles;                       // (sample, chunk of tokens), or rt samples
+  const int64_t col = ((int64_t)(blockIdx.x - unit * a.col_tiles) * ct + c) * N, left = a.d - col;
+  int64_t row0, row1;                                                  // rows of [B * T]
+  if constexpr (TOKEN) {
+    row0 = unit * rt;
+    row1 = row0 + rt < a.B ? row0 + rt : a.B;
+  } else {
+    const int64_t i = unit / a.chunks, k = unit - i * a.chunks;
+    row0 = i * a.T + k * a.rows_per_chunk;
+    row1 = (k + 1) * a.rows_per_chunk < a.T ? row0 + a.rows_per_chunk : (i + 1) * a.T;
+  }
+  const int64_t nb = checkpoint8_blocks(a.d);
+  float sum[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum[k] = 0.0f;
+  if (left > 0) {
+    for (int64_t row = row0 + r; row < row1; row += (int64_t)rt * UNROLL) {
+      u32x4_t dy[UNROLL], zr[UNROLL];
+      uint32_t zq[UNROLL][N / 4];
+      int sc[UNROLL];
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        const int64_t rw = row + (int64_t)u * rt;
+        if (rw < row1) {
+          dy[u] = load_chunk<DT>((const char*)a.dY + rw * a.d * Chunk<DT>::BYTES, col, left);
+          if constexpr (ZK == Z_SAME) zr[u] = load_chunk<DT>((const char*)a.Z + rw * a.d * Chunk<DT>::BYTES, col, left);
+          if constexpr (ZK == Z_EIGHT) {
+            load_q<N>((const signed char*)a.Z + rw * a.d + col, left, zq[u]);
+            sc[u] = a.scales[rw * nb + col / CKPT8_BLOCK];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        const int64_t rw = row + (int64_t)u * rt;
+        if (rw < row1) {
+          float f[N], z[N];
+          widen_chunk<DT>(dy[u], f);
+          if constexpr (ZK == Z_SAME) widen_chunk<DT>(zr[u], z);
+          if constexpr (ZK == Z_EIGHT) {
+            const float scale = power_of_two(sc[u] - 127);
+#pragma unroll
+            for (int k = 0; k < N; ++k) z[k] = checkpoint8_value(zq[u][k >> 2], k & 3, scale);
+          }
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            if constexpr (ZK != Z_NONE) f[k] *= act_slope<ACT>(z[k]);
+            sum[k] += f[k];
+          }
+          if (a.dZ) store_chunk<DT>((char*)a.dZ + rw * a.d * Chunk<DT>::BYTES, col, left, round_chunk<DT>(f));
+          if constexpr (TOKEN) {
+            if (a.partial) {
+#pragma unroll
+              for (int q = 0; q < N / 4; ++q)
+                store_chunk<DT_F32>(a.partial + rw * a.d, col + 4 * q, left - 4 * q,
+                                    u32x4_t{__builtin_bit_cast(uint32_t, f[4 * q]), __builtin_bit_cast(uint32_t, f[4 * q + 1]),
+                                            __builtin_bit_cast(uint32_t, f[4 * q + 2]), __builtin_bit_cast(uint32_t, f[4 * q + 3])});
+            }
+          }
+        }
+      }
+    }
+  }
+  if constexpr (!TOKEN) {
+    if (!a.partial) return;
+#pragma unroll
+    for (int k = 0; k < N; ++k) part[k * 256 + threadIdx.x] = sum[k];
+    __syncthreads();
+    // element e of the column tile: its N ct sums lie at [e % N][.. e / N ..]; one thread per element, neighbours side by side
+    float* to = a.partial + unit * a.d;
+    const int64_t first = (int64_t)(blockIdx.x - unit * a.col_tiles) * ct * N;
+    for (int e = threadIdx.x; e < ct * N; e += 256) {
+      if (first + e >= a.d) break;
+      const float* p = part + (e % N) * 256 + e / N;
+      float s = 0.0f;
+      for (int k = 0; k < rt; ++k) s += p[k * ct];
+      to[first + e] = s;
+    }
+  }
+}
+
+}  // namespace flashdp

@@ -1,0 +1,46 @@
+// The activations of the linear layers' epilogue and their slopes, in fp32.
+//
+// All but ReLU are z times a smooth step, and each is written so that the step keeps its relative accuracy where it is small
+// (for z << 0), without a cancelling 1 + tanh or 1 + erf:
+//   GELU (tanh form)  z s(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3), since (1 + tanh u) / 2 is the logistic function s of 2 u
+//   SiLU              z s(z)
+//   GELU              z erfc(-z / sqrt(2)) / 2
+// s(v) = 1 / (1 + e^-v): for v << 0 the exponential overflows to infinity and s is 0.  All of them have reached their limits
+// in fp32 at |z| = 128, where arguments are cut off, so that infinities give the limit and not 0 times infinity; NaN
+// stays NaN (every comparison with it is false).
+#pragma once
+#include <hip/hip_runtime.h>
+
+namespace flashdp {
+
+enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4 };
+
+__device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+  if constexpr (ACT == ACT_NONE) return z;
+  if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : z;
+  z = z < -128.0f ? -128.0f : z;
+  if constexpr (ACT == ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+  if constexpr (ACT == ACT_GELU_TANH) return z * logistic(1.5957691f * z * fmaf(0.044715f * z, z, 1.0f));
+  if constexpr (ACT == ACT_SILU) return z * logistic(z);
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if constexpr (ACT == ACT_NONE) return 1.0f;
+  if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : z > 0.0f ? 1.0f : z;
+  z = z < -128.0f ? -128.0f : z > 128.0f ? 128.0f : z;
+  if constexpr (ACT == ACT_GELU) return fmaf(0.39894228f * z, __expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678f * z));
+  if constexpr (ACT == ACT_GELU_TANH) {
+    const float zz = z * z, s = logistic(1.5957691f * z * fmaf(0.044715f, zz, 1.0f));
+    return fmaf(z * 1.5957691f * fmaf(3.0f * 0.044715f, zz, 1.0f) * (1.0f - s), s, s);   // s + z s (1 - s) d(2 u)/dz
+  }
+  if constexpr (ACT == ACT_SILU) {
+    const float s = logistic(z);
+    return fmaf(z * (1.0f - s), s, s);
+  }
+}
+
+}  // namespace flashdp

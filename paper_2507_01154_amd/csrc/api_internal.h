@@ -1,0 +1,20 @@
+// What the translation units of the library share on the host: the device check, the library-owned workspace and the
+// thread's record of what a call took (all defined in flashdp_api.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace flashdp {
+namespace api {
+
+__attribute__((visibility("hidden"))) int current_device(int* dev);
+// At least `need` bytes of the library-owned workspace of the current device, grown if need be - but not while `stream` is
+// being captured, where FLASHDP_WORKSPACE_TOO_SMALL is the answer instead.
+__attribute__((visibility("hidden"))) int library_workspace(size_t need, hipStream_t stream, void** ptr);
+__attribute__((visibility("hidden"))) int64_t compute_units();
+__attribute__((visibility("hidden"))) void note_kernel(const char* name);
+__attribute__((visibility("hidden"))) hipError_t allow_lds(const void* kernel, int bytes);
+
+}  // namespace api
+}  // namespace flashdp

@@ -1,0 +1,124 @@
+// Activations in 8 bits between forward and backward pass.
+//
+// Blocks of 32 consecutive features of a row share an exponent e, an element is q 2^e, -127 <= q <= 127:
+//   m = largest finite magnitude of the block, e = max(floor(log2 m) - 6, least), q = clamp(round(x 2^-e), -127, 127).
+// So 64 <= m 2^-e < 128: an element is off by at most 2^e / 2 <= m / 128 (the clamp cuts what rounds to 128, which is then off by
+// less than 2^e).  A power of two as scale, at the cost of up to one bit of resolution, makes both directions exact but for the
+// one rounding: x 2^-e is exact in fp32, ties included, and q 2^e has 7 significant bits, so it is exact in bfloat16, fp16 and fp32
+// alike and the backward pass contracts the very values that were kept.  The scale depends on one row alone: a sample's gradient
+// is a function of that sample only, which the clipping needs.
+// least = -126 keeps 2^e and 2^-e normal numbers (blocks below 2^-120 lose resolution); for fp16 -24, the step of its subnormals,
+// of which every fp16 number is a multiple.  An element that is not finite is kept as q = -128 and comes back as NaN.
+// Layout: q of all rows, [rows][d] int8, up to a multiple of 16 bytes; then e + 127 of all blocks, [rows][ceil(d / 32)] uint8.
+//
+// Memory bound: 2 (4) + 33/32 bytes an element.  Four lanes (fp32: eight) hold a block and agree on m by exchanges inside the wave.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "vector_io.hip.h"
+
+namespace flashdp {
+
+constexpr int CKPT8_BLOCK = 32;
+
+__host__ __device__ __forceinline__ int64_t checkpoint8_blocks(int64_t d) { return (d + CKPT8_BLOCK - 1) / CKPT8_BLOCK; }
+__host__ __device__ __forceinline__ int64_t checkpoint8_scales_at(int64_t rows, int64_t d) { return (rows * d + 15) / 16 * 16; }
+
+template <int DT> struct Checkpoint8Least { static constexpr int EXP = DT == DT_F16 ? -24 : -126; };
+
+__device__ __forceinline__ bool finite_f32(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7F800000u) != 0x7F800000u; }
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+// e of a block whose largest finite magnitude is m
+template <int DT>
+__device__ __forceinline__ int checkpoint8_exponent(float m) {
+  const int e = (int)(__builtin_bit_cast(uint32_t, m) >> 23) - 127 - 6;
+  return e < Checkpoint8Least<DT>::EXP ? Checkpoint8Least<DT>::EXP : e;
+}
+// q of x in a block of scale 2^-e = inv, in the low byte
+__device__ __forceinline__ uint32_t checkpoint8_quantise(float x, float inv) {
+  const float r = fminf(fmaxf(__builtin_rintf(x * inv), -127.0f), 127.0f);
+  const int q = (int)r;
+  return finite_f32(x) ? (uint32_t)q & 0xFFu : 0x80u;
+}
+// the value of byte k (0..3) of four q, scale 2^e
+__device__ __forceinline__ float checkpoint8_value(uint32_t q4, int k, float scale) {
+  const int q = (int)(q4 << (24 - 8 * k)) >> 24;
+  return q == -128 ? __builtin_bit_cast(float, 0x7FC00000u) : (float)q * scale;
+}
+
+typedef uint32_t u32_any_t __attribute__((aligned(1)));
+
+// Up to n bytes of q (n = 8 or 4, one chunk) at q[col ..], `left` of which exist; what does not exist reads as zero.
+template <int N>
+__device__ __forceinline__ void load_q(const signed char* q, int64_t left, uint32_t (&v)[N / 4]) {
+  if (left >= N) {
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) v[k] = ((const u32_any_t*)q)[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) v[k] = 0u;
+#pragma unroll
+    for (int k = 0; k < N - 1; ++k)
+      if (k < left) v[k >> 2] |= (uint32_t)(unsigned char)q[k] << (8 * (k & 3));
+  }
+}
+
+// One thread per chunk of 16 bytes of x; the chunks of a row fill whole blocks (chunks past the row's end hold zeros and store
+// nothing), so the lanes of a block are neighbours in one wave.
+template <int DT>
+__global__ __launch_bounds__(256) void checkpoint8_pack_kernel(const void* x, int64_t rows, int64_t d, signed char* q, unsigned char* scales) {
+  constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;   // chunks per block
+  const int64_t nb = checkpoint8_blocks(d), chunks = rows * nb * PER;
+  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const bool in = c < chunks;
+  const int64_t block = in ? c / PER : 0, row = block / nb, b = block - row * nb;
+  const int64_t col = b * CKPT8_BLOCK + (c % PER) * N, left = in ? d - col : 0;
+  float f[N];
+  widen_chunk<DT>(load_chunk<DT>((const char*)x + row * d * Chunk<DT>::BYTES, col, left), f);
+  float m = 0.0f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = fmaxf(m, finite_f32(f[k]) ? fabsf(f[k]) : 0.0f);
+#pragma unroll
+  for (int off = 1; off < PER; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if (left <= 0) return;
+  const int e = checkpoint8_exponent<DT>(m);
+  const float inv = power_of_two(-e);
+  uint32_t v[N / 4];
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k)
+    v[k] = checkpoint8_quantise(f[4 * k], inv) | checkpoint8_quantise(f[4 * k + 1], inv) << 8 |
+           checkpoint8_quantise(f[4 * k + 2], inv) << 16 | checkpoint8_quantise(f[4 * k + 3], inv) << 24;
+  signed char* to = q + row * d + col;
+  if (left >= N) {
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) ((u32_any_t*)to)[k] = v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < N - 1; ++k)
+      if (k < left) to[k] = (signed char)(v[k >> 2] >> (8 * (k & 3)));
+  }
+  if (c % PER == 0) scales[block] = (unsigned char)(e + 127);
+}
+
+// And back.
+template <int DT>
+__global__ __launch_bounds__(256) void checkpoint8_unpack_kernel(const signed char* q, const unsigned char* scales, int64_t rows, int64_t d, void* x) {
+  constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;
+  const int64_t nb = checkpoint8_blocks(d), chunks = rows * nb * PER;
+  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (c >= chunks) return;
+  const int64_t block = c / PER, row = block / nb, b = block - row * nb;
+  const int64_t col = b * CKPT8_BLOCK + (c % PER) * N, left = d - col;
+  if (left <= 0) return;
+  uint32_t v[N / 4];
+  load_q<N>(q + row * d + col, left, v);
+  const float scale = power_of_two((int)scales[block] - 127);
+  float f[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) f[k] = checkpoint8_value(v[k >> 2], k & 3, scale);
+  store_chunk<DT>((char*)x + row * d * Chunk<DT>::BYTES, col, left, round_chunk<DT>(f));
+}
+
+}  // namespace flashdp

@@ -14,6 +14,7 @@
 #include <mutex>
 #include <vector>
 
+#include "api_internal.h"
 #include "elementwise.hip.h"
 #include "gemm_mfma.hip.h"
 #include "gemm_mfma_dma.hip.h"
@@ -1115,6 +1116,22 @@ int run_layer(const flashdp_layer_t& L0, int64_t B, int64_t T, int dtype, int mo
 }
 
 }  // namespace
+
+namespace flashdp {
+namespace api {
+
+int current_device(int* dev) { return device_or_error(dev); }
+int library_workspace(size_t need, hipStream_t stream, void** ptr) {
+  size_t got = 0;
+  const int st = owned_workspace(need, ptr, &got, 0, 0, stream);
+  return st != FLASHDP_OK ? st : got < need ? FLASHDP_WORKSPACE_TOO_SMALL : FLASHDP_OK;
+}
+int64_t compute_units() { return plan_cus(); }
+void note_kernel(const char* name) { g_ctx.last_kernel = name; }
+hipError_t allow_lds(const void* kernel, int bytes) { return ensure_lds_limit(kernel, bytes); }
+
+}  // namespace api
+}  // namespace flashdp
 
 extern "C" {
 

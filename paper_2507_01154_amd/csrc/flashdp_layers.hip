@@ -1,0 +1,416 @@
+// C ABI of the layers around the DP weight gradient (see include/flashdp.h): the forward product with its epilogue, the backward pass
+// of activation and bias, layer normalisation, 8-bit checkpoints.  Host code validates, sizes workspaces, picks kernels and
+// enqueues them.
+#include "../../include/flashdp.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "activation_dp.hip.h"
+#include "api_internal.h"
+#include "checkpoint8.hip.h"
+#include "forward_tile.hip.h"
+#include "layernorm.hip.h"
+#include "vector_dp.hip.h"
+
+using namespace flashdp;
+
+namespace {
+
+#define HIP_TRY(expr) do { if ((expr) != hipSuccess) { (void)hipGetLastError(); return FLASHDP_HIP_ERROR; } } while (0)
+
+constexpr int64_t GRID_LIMIT = (int64_t(1) << 31) - 1;
+constexpr int64_t FEATURE_LIMIT = int64_t(1) << 30;      // columns are computed in 32 bits
+constexpr int64_t ROW_LIMIT = int64_t(1) << 40;
+
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline bool valid_dtype(int d) { return d == FLASHDP_BF16 || d == FLASHDP_F32 || d == FLASHDP_F16; }
+inline bool valid_act(int a) { return a >= FLASHDP_ACT_NONE && a <= FLASHDP_ACT_SILU; }
+inline bool valid_clip(float C, float sigma) { return C > 0.0f && std::isfinite(C) && sigma >= 0.0f && std::isfinite(sigma); }
+
+int check_rows(int64_t rows, int64_t d) {
+  if (rows <= 0 || d <= 0) return FLASHDP_INVALID_ARGUMENT;
+  return rows >= ROW_LIMIT || d > FEATURE_LIMIT ? FLASHDP_UNSUPPORTED_SHAPE : FLASHDP_OK;
+}
+int check_samples(int64_t B, int64_t T, int64_t d) {
+  if (B <= 0 || T <= 0 || d <= 0) return FLASHDP_INVALID_ARGUMENT;
+  return B >= (int64_t(1) << 20) || T >= (int64_t(1) << 31) || B * T >= ROW_LIMIT || d > FEATURE_LIMIT ? FLASHDP_UNSUPPORTED_SHAPE : FLASHDP_OK;
+}
+
+// f(integral_constant<DT>) for the storage type of a call
+template <typename F>
+auto by_dtype(int dtype, F&& f) {
+  if (dtype == FLASHDP_BF16) return f(std::integral_constant<int, DT_BF16>{});
+  if (dtype == FLASHDP_F16) return f(std::integral_constant<int, DT_F16>{});
+  return f(std::integral_constant<int, DT_F32>{});
+}
+inline int chunk_elements(int dtype) { return dtype == FLASHDP_F32 ? 4 : 8; }
+
+template <typename... Formal, typename... Actual>
+hipError_t launch(void (*kernel)(Formal...), int64_t grid, int threads, size_t lds, hipStream_t st, Actual... args) {
+  if (grid <= 0 || grid > GRID_LIMIT) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3((unsigned)threads), lds, st, args...);
+  return hipGetLastError();
+}
+
+// ---- per-sample gradients of vectors ----------------------------------------------------------------
+
+struct VectorWs { size_t partial, g, squares, factors, total; int blocks; };
+
+VectorWs vector_ws(int64_t B, int64_t chunks, int64_t n) {
+  VectorWs w;
+  w.blocks = (int)((n + 63) / 64);
+  w.partial = 0;
+  w.g = align_up((size_t)B * chunks * n * 4, 256);
+  w.squares = w.g + (chunks > 1 ? align_up((size_t)B * n * 4, 256) : 0);
+  w.factors = w.squares + align_up((size_t)B * w.blocks * 8, 256);
+  w.total = w.factors + align_up((size_t)B * 4, 256);
+  return w;
+}
+
+// What comes after the partial sums: their sum, norms, clip factors, the clipped sum and its noise.
+hipError_t run_vector(VectorArgs& v, char* ws, const VectorWs& w, hipStream_t st) {
+  v.partial = reinterpret_cast<const float*>(ws + w.partial);
+  v.g = reinterpret_cast<float*>(ws + (v.chunks > 1 ? w.g : w.partial));
+  v.squares = reinterpret_cast<double*>(ws + w.squares);
+  v.factors = reinterpret_cast<float*>(ws + w.factors);
+  v.blocks = w.blocks;
+  hipError_t e = launch(vector_sum_kernel, v.B * v.blocks, 256, 0, st, v);
+  if (e != hipSuccess) return e;
+  const int64_t grid = (v.n + 15) / 16;
+  if (v.B <= VECTOR_FOLD_B && v.B * v.blocks <= VECTOR_FOLD_SQUARES) return launch(vector_clip_kernel<true>, grid, 256, 0, st, v);
+  e = launch(vector_factors_kernel, (v.B + 3) / 4, 256, 0, st, v);
+  return e != hipSuccess ? e : launch(vector_clip_kernel<false>, grid, 256, 0, st, v);
+}
+
+// Tokens per partial sum: about four workgroups per compute unit (column_groups of them per chunk of tokens), and no fewer than
+// 16 tokens, below which writing and reading the partial sums shows.
+int64_t chunks_of(int64_t B, int64_t T, int64_t column_groups) {
+  const int64_t want = (4 * 256 + B * column_groups - 1) / (B * column_groups);
+  return std::max<int64_t>(1, std::min(want, (T + 15) / 16));
+}
+
+struct ActivationPlan { int log_ct; int64_t col_tiles, chunks, rows_per_chunk; bool token; };
+
+ActivationPlan activation_plan(int64_t B, int64_t T, int64_t d, int dtype) {
+  ActivationPlan p;
+  const int64_t columns = (d + chunk_elements(dtype) - 1) / chunk_elements(dtype);
+  p.log_ct = 3;
+  while (p.log_ct < 6 && (int64_t(1) << p.log_ct) < columns) ++p.log_ct;
+  p.col_tiles = (columns + (1 << p.log_ct) - 1) >> p.log_ct;
+  p.token = T == 1;
+  const int64_t k = p.token ? 1 : chunks_of(B, T, p.col_tiles);
+  p.rows_per_chunk = (T + k - 1) / k;
+  p.chunks = (T + p.rows_per_chunk - 1) / p.rows_per_chunk;
+  return p;
+}
+
+template <int DT, int ZK>
+auto activation_kernel(int act, bool token) {
+  if constexpr (ZK == Z_NONE) return token ? activation_dp_kernel<DT, ACT_NONE, ZK, true> : activation_dp_kernel<DT, ACT_NONE, ZK, false>;
+  else switch (act) {
+    case FLASHDP_ACT_RELU: return token ? activation_dp_kernel<DT, ACT_RELU, ZK, true> : activation_dp_kernel<DT, ACT_RELU, ZK, false>;
+    case FLASHDP_ACT_GELU: return token ? activation_dp_kernel<DT, ACT_GELU, ZK, true> : activation_dp_kernel<DT, ACT_GELU, ZK, false>;
+    case FLASHDP_ACT_GELU_TANH: return token ? activation_dp_kernel<DT, ACT_GELU_TANH, ZK, true> : activation_dp_kernel<DT, ACT_GELU_TANH, ZK, false>;
+    default: return token ? activation_dp_kernel<DT, ACT_SILU, ZK, true> : activation_dp_kernel<DT, ACT_SILU, ZK, false>;
+  }
+}
+
+// ---- layer normalisation ----------------------------------------------------------------------------
+
+// Chunks of 16 bytes a row has decide who holds it: a wave up to 4 chunks a lane, a workgroup up to 8, nobody beyond.
+constexpr int64_t NORM_LONG = 256 * 8;
+
+template <int DT>
+void (*norm_kernel(int64_t columns))(const NormArgs) {
+  if (columns <= 64) return layernorm_forward_kernel<DT, 64, 1>;
+  if (columns <= 128) return layernorm_forward_kernel<DT, 64, 2>;
+  if (columns <= 256) return layernorm_forward_kernel<DT, 64, 4>;
+  if (columns <= 512) return layernorm_forward_kernel<DT, 256, 2>;
+  if (columns <= 768) return layernorm_forward_kernel<DT, 256, 3>;
+  if (columns <= 1024) return layernorm_forward_kernel<DT, 256, 4>;
+  return layernorm_forward_kernel<DT, 256, 8>;
+}
+template <int DT>
+void (*norm_grad_kernel(int64_t columns))(const NormGradArgs) {
+  if (columns <= 64) return layernorm_grad_kernel<DT, 64, 1>;
+  if (columns <= 128) return layernorm_grad_kernel<DT, 64, 2>;
+  if (columns <= 256) return layernorm_grad_kernel<DT, 64, 4>;
+  if (columns <= 512) return layernorm_grad_kernel<DT, 256, 2>;
+  if (columns <= 768) return layernorm_grad_kernel<DT, 256, 3>;
+  if (columns <= 1024) return layernorm_grad_kernel<DT, 256, 4>;
+  return layernorm_grad_kernel<DT, 256, 8>;
+}
+
+struct NormPlan { int64_t columns, col_tiles, chunks, rows_per_chunk; };
+
+NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
+  NormPlan p;
+  p.columns = (d + chunk_elements(dtype) - 1) / chunk_elements(dtype);
+  p.col_tiles = p.columns > NORM_LONG ? (p.columns + 255) / 256 : 1;
+  const int64_t k = chunks_of(B, T, p.col_tiles);
+  p.rows_per_chunk = (T + k - 1) / k;
+  p.chunks = (T + p.rows_per_chunk - 1) / p.rows_per_chunk;
+  return p;
+}
+
+using Tile128x128 = ForwardTileCfg<128, 128>;
+using Tile64x64 = ForwardTileCfg<64, 64>;
+
+template <typename Cfg, int DT>
+hipError_t launch_forward_tile(ForwardArgs& a, hipStream_t st) {
+  const int64_t tm = (a.rows + Cfg::BM - 1) / Cfg::BM, tn = ((int64_t)a.D + Cfg::BN - 1) / Cfg::BN;
+  if (tm * 8 > GRID_LIMIT || tn * 8 > GRID_LIMIT || tm * tn > GRID_LIMIT) return hipErrorInvalidValue;
+  a.tiles_m = (int)tm; a.tiles_n = (int)tn;
+  const hipError_t e = api::allow_lds(reinterpret_cast<const void*>(forward_tile_kernel<Cfg, DT>), Cfg::LDS_BYTES);
+  return e != hipSuccess ? e : launch(forward_tile_kernel<Cfg, DT>, tm * tn, Cfg::NT, Cfg::LDS_BYTES, st, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int flashdp_linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t rows, int64_t d_in, int64_t d_out,
+                           int dtype, int activation, void* Y, void* Z, int z_8bit, void* stream) {
+  if (!X || !W || !Y || !valid_dtype(dtype) || !valid_act(activation) || (z_8bit != 0 && z_8bit != 1) || (z_8bit && !Z)) return FLASHDP_INVALID_ARGUMENT;
+  int st = check_rows(rows, d_in);
+  if (st == FLASHDP_OK) st = check_rows(rows, d_out);
+  if (st != FLASHDP_OK) return st;
+  // (grid of the smallest tiles)
+  if ((rows + 63) / 64 * 8 > GRID_LIMIT || (rows + 63) / 64 * ((d_out + 63) / 64) > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(Z, 16)) return FLASHDP_MISALIGNED;
+  int dev = 0;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
+  ForwardArgs a;
+  a.X = X; a.W = W; a.bias = bias; a.residual = residual; a.Y = Y; a.Z = Z;
+  a.scales = z_8bit ? static_cast<unsigned char*>(Z) + checkpoint8_scales_at(rows, d_out) : nullptr;
+  a.rows = rows; a.K = (int)d_in; a.D = (int)d_out;
+  a.act = activation; a.keep = !Z ? KEEP_NONE : z_8bit ? KEEP_EIGHT : KEEP_SAME;
+  a.tiles_m = a.tiles_n = 0;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  const bool large = ((rows + 127) / 128) * ((d_out + 127) / 128) >= 256;
+  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    return large ? launch_forward_tile<Tile128x128, DT>(a, hs) : launch_forward_tile<Tile64x64, DT>(a, hs);
+  }));
+  api::note_kernel("forward_tile_kernel");
+  return FLASHDP_OK;
+}
+
+size_t flashdp_activation_workspace_bytes(int64_t B, int64_t T, int64_t d_out, int dtype) {
+  if (!valid_dtype(dtype) || check_samples(B, T, d_out) != FLASHDP_OK) return 0;
+  return vector_ws(B, activation_plan(B, T, d_out, dtype).chunks, d_out).total;
+}
+
+int flashdp_activation_dp_grad(const void* dY, const void* Z, int z_8bit, int64_t B, int64_t T, int64_t d_out, int dtype, int activation,
+                               float C, float sigma, uint64_t seed, uint32_t layer, void* dZ, float* out_grad, float* out_norms,
+                               void* workspace, size_t workspace_bytes, void* stream, int accumulate, int add_noise) {
+  if (!dY || !valid_dtype(dtype) || !valid_act(activation) || (z_8bit != 0 && z_8bit != 1) || (!dZ && !out_grad)) return FLASHDP_INVALID_ARGUMENT;
+  if (activation != FLASHDP_ACT_NONE && !Z) return FLASHDP_INVALID_ARGUMENT;
+  if (out_grad && !valid_clip(C, sigma)) return FLASHDP_INVALID_ARGUMENT;
+  int st = check_samples(B, T, d_out);
+  if (st != FLASHDP_OK) return st;
+  const bool use_z = activation != FLASHDP_ACT_NONE;
+  if (!aligned(dY, 16) || (use_z && !aligned(Z, 16)) || !aligned(dZ, 16) || !aligned(out_grad, 16) || !aligned(out_norms, 4) || !aligned(workspace, 16))
+    return FLASHDP_MISALIGNED;
+  const ActivationPlan p = activation_plan(B, T, d_out, dtype);
+  const int64_t rt = 256 >> p.log_ct, units = p.token ? (B + rt - 1) / rt : B * p.chunks;
+  const VectorWs w = vector_ws(B, p.chunks, d_out);
+  if (units * p.col_tiles > GRID_LIMIT || B * w.blocks > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  if (out_grad && workspace && workspace_bytes < w.total) return FLASHDP_WORKSPACE_TOO_SMALL;
+  int dev = 0;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (out_grad && !workspace && (st = api::library_workspace(w.total, hs, &workspace)) != FLASHDP_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  ActivationArgs a;
+  a.dY = dY; a.Z = Z; a.dZ = dZ;
+  a.scales = use_z && z_8bit ? static_cast<const unsigned char*>(Z) + checkpoint8_scales_at(B * T, d_out) : nullptr;
+  a.partial = out_grad ? reinterpret_cast<float*>(ws + w.partial) : nullptr;
+  a.B = B; a.T = T; a.d = d_out;
+  a.chunks = (int)p.chunks; a.rows_per_chunk = (int)p.rows_per_chunk; a.col_tiles = (int)p.col_tiles; a.log_ct = p.log_ct;
+  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    auto kernel = !use_z ? activation_kernel<DT, Z_NONE>(activation, p.token) : z_8bit ? activation_kernel<DT, Z_EIGHT>(activation, p.token)
+                                                                                       : activation_kernel<DT, Z_SAME>(activation, p.token);
+    return launch(kernel, units * p.col_tiles, 256, 0, hs, a);
+  }));
+  api::note_kernel("activation_dp_kernel");
+  if (!out_grad) return FLASHDP_OK;
+  VectorArgs v;
+  v.n = d_out; v.B = B; v.chunks = a.chunks;
+  v.C = C; v.noise_scale = add_noise ? sigma * C : 0.0f; v.seed = seed; v.layer = layer; v.field = FLASHDP_FIELD_BIAS;
+  v.out = out_grad; v.out_norms = out_norms; v.accumulate = accumulate ? 1 : 0;
+  HIP_TRY(run_vector(v, ws, w, hs));
+  return FLASHDP_OK;
+}
+
+int flashdp_layernorm_forward(const void* X, const void* gamma, const void* beta, int64_t rows, int64_t d, int dtype, float eps, void* Y,
+                              float* mean, float* rstd, void* stream) {
+  if (!X || !gamma || !Y || !valid_dtype(dtype) || !(eps > 0.0f) || !std::isfinite(eps)) return FLASHDP_INVALID_ARGUMENT;
+  int st = check_rows(rows, d);
+  if (st != FLASHDP_OK) return st;
+  if (rows > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  if (!aligned(X, 16) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(Y, 16) || !aligned(mean, 4) || !aligned(rstd, 4)) return FLASHDP_MISALIGNED;
+  int dev = 0;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
+  NormArgs a;
+  a.X = X; a.gamma = gamma; a.beta = beta; a.Y = Y; a.mean = mean; a.rstd = rstd; a.rows = rows; a.d = d; a.eps = eps;
+  const int64_t columns = (d + chunk_elements(dtype) - 1) / chunk_elements(dtype);
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    if (columns > NORM_LONG) return launch(layernorm_forward_long_kernel<DT>, rows, 256, 0, hs, a);
+    return launch(norm_kernel<DT>(columns), columns <= 256 ? (rows + 3) / 4 : rows, 256, 0, hs, a);
+  }));
+  api::note_kernel(columns > NORM_LONG ? "layernorm_forward_long_kernel" : "layernorm_forward_kernel");
+  return FLASHDP_OK;
+}
+
+size_t flashdp_layernorm_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype, int bias) {
+  if (!valid_dtype(dtype) || check_samples(B, T, d) != FLASHDP_OK) return 0;
+  return vector_ws(B, norm_plan(B, T, d, dtype).chunks, bias ? 2 * d : d).total;
+}
+
+int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, const float* mean, const float* rstd, int64_t B, int64_t T, int64_t d,
+                              int dtype, float C, float sigma, uint64_t seed, uint32_t layer, void* dX, float* out_grad, float* out_norms, int bias,
+                              void* workspace, size_t workspace_bytes, void* stream, int accumulate, int add_noise) {
+  if (!X || !dY || !gamma || !mean || !rstd || !valid_dtype(dtype) || (!dX && !out_grad)) return FLASHDP_INVALID_ARGUMENT;
+  if (out_grad && !valid_clip(C, sigma)) return FLASHDP_INVALID_ARGUMENT;
+  int st = check_samples(B, T, d);
+  if (st != FLASHDP_OK) return st;
+  if (!aligned(X, 16) || !aligned(dY, 16) || !aligned(gamma, 16) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dX, 16) || !aligned(out_grad, 16) ||
+      !aligned(out_norms, 4) || !aligned(workspace, 16))
+    return FLASHDP_MISALIGNED;
+  const int64_t n = bias ? 2 * d : d;
+  const NormPlan p = norm_plan(B, T, d, dtype);
+  const VectorWs w = vector_ws(B, p.chunks, n);
+  if (B * p.chunks * p.col_tiles > GRID_LIMIT || B * w.blocks > GRID_LIMIT || (p.columns > NORM_LONG && B * T > GRID_LIMIT)) return FLASHDP_UNSUPPORTED_SHAPE;
+  if (out_grad && workspace && workspace_bytes < w.total) return FLASHDP_WORKSPACE_TOO_SMALL;
+  int dev = 0;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (out_grad && !workspace && (st = api::library_workspace(w.total, hs, &workspace)) != FLASHDP_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  NormGradArgs a;
+  a.X = X; a.dY = dY; a.gamma = gamma; a.mean = mean; a.rstd = rstd; a.dX = dX;
+  a.partial = out_grad ? reinterpret_cast<float*>(ws + w.partial) : nullptr;
+  a.T = T; a.d = d; a.chunks = (int)p.chunks; a.rows_per_chunk = (int)p.rows_per_chunk; a.bias = bias ? 1 : 0;
+  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    if (p.columns <= NORM_LONG) return launch(norm_grad_kernel<DT>(p.columns), B * p.chunks, 256, 0, hs, a);
+    hipError_t e = hipSuccess;
+    if (out_grad) e = launch(layernorm_grad_long_sums_kernel<DT>, B * p.chunks * p.col_tiles, 256, 0, hs, a, (int)p.col_tiles);
+    if (e == hipSuccess && dX) e = launch(layernorm_grad_long_rows_kernel<DT>, B * T, 256, 0, hs, a);
+    return e;
+  }));
+  api::note_kernel(p.columns <= NORM_LONG ? "layernorm_grad_kernel" : "layernorm_grad_long_rows_kernel");
+  if (!out_grad) return FLASHDP_OK;
+  VectorArgs v;
+  v.n = n; v.B = B; v.chunks = a.chunks;
+  v.C = C; v.noise_scale = add_noise ? sigma * C : 0.0f; v.seed = seed; v.layer = layer; v.field = FLASHDP_FIELD_NORM;
+  v.out = out_grad; v.out_norms = out_norms; v.accumulate = accumulate ? 1 : 0;
+  HIP_TRY(run_vector(v, ws, w, hs));
+  return FLASHDP_OK;
+}
+
+size_t flashdp_checkpoint8_bytes(int64_t rows, int64_t d) {
+  if (check_rows(rows, d) != FLASHDP_OK) return 0;
+  return (size_t)(checkpoint8_scales_at(rows, d) + rows * checkpoint8_blocks(d));
+}
+
+int flashdp_checkpoint8_pack(const void* X, int64_t rows, int64_t d, int dtype, void* packed, void* stream) {
+  if (!X || !packed || !valid_dtype(dtype)) return FLASHDP_INVALID_ARGUMENT;
+  int st = check_rows(rows, d);
+  if (st != FLASHDP_OK) return st;
+  if (!aligned(X, 16) || !aligned(packed, 16)) return FLASHDP_MISALIGNED;
+  const int64_t grid = (rows * checkpoint8_blocks(d) * (CKPT8_BLOCK / chunk_elements(dtype)) + 255) / 256;
+  if (grid > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  int dev = 0;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
+  signed char* q = static_cast<signed char*>(packed);
+  unsigned char* scales = static_cast<unsigned char*>(packed) + checkpoint8_scales_at(rows, d);
+  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+    return launch(checkpoint8_pack_kernel<decltype(dt)::value>, grid, 256, 0, static_cast<hipStream_t>(stream), X, rows, d, q, scales);
+  }));
+  return FLASHDP_OK;
+}
+
+int flashdp_checkpoint8_unpack(const void* packed, int64_t rows, int64_t d, int dtype, void* X, void* stream) {
+  if (!X || !packed || !valid_dtype(dtype)) return FLASHDP_INVALID_ARGUMENT;
+  int st = check_rows(rows, d);
+  if (st != FLASHDP_OK) return st;
+  if (!aligned(X, 16) || !aligned(packed, 16)) return FLASHDP_MISALIGNED;
+  const int64_t grid = (rows * checkpoint8_blocks(d) * (CKPT8_BLOCK / chunk_elements(dtype)) + 255) / 256;
+  if (grid > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  int dev = 0;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
+  const signed char* q = static_cast<const signed char*>(packed);
+  const unsigned char* scales = static_cast<const unsigned char*>(packed) + checkpoint8_scales_at(rows, d);
+  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+    return launch(checkpoint8_unpack_kernel<decltype(dt)::value>, grid, 256, 0, static_cast<hipStream_t>(stream), q, scales, rows, d, X);
+  }));
+  return FLASHDP_OK;
+}
+
+// Room for the unpacked activation of one layer, in front of the schedule's own workspace.
+static size_t unpacked_bytes(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype) {
+  size_t most = 0;
+  for (int l = 0; l < n_layers; ++l) most = std::max(most, (size_t)B * T * layers[l].d_in * (dtype == FLASHDP_F32 ? 4 : 2));
+  return align_up(most, 256);
+}
+
+size_t flashdp_workspace_bytes_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule) {
+  const size_t need = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, schedule);
+  return need == 0 ? 0 : unpacked_bytes(layers, n_layers, B, T, dtype) + need;
+}
+
+int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule, void* workspace,
+                                      size_t workspace_bytes, void* stream, int accumulate, int add_noise) {
+  if (!layers || n_layers <= 0 || !valid_dtype(dtype) || schedule < FLASHDP_SCHEDULE_AUTO || schedule > FLASHDP_SCHEDULE_FUSED) return FLASHDP_INVALID_ARGUMENT;
+  // the layers as the ordinary call will see them; it repeats these checks, but after a layer has been unpacked
+  for (int l = 0; l < n_layers; ++l) {
+    const flashdp_layer_t& L = layers[l];
+    if (!L.X || !L.dY || !L.out_grad || !valid_clip(L.C, L.sigma)) return FLASHDP_INVALID_ARGUMENT;
+    if (!aligned(L.X, 16) || !aligned(L.dY, 16) || !aligned(L.out_grad, 16) || !aligned(L.out_norms, 4)) return FLASHDP_MISALIGNED;
+  }
+  if (!aligned(workspace, 16)) return FLASHDP_MISALIGNED;
+  if (B <= 0 || T <= 0) return FLASHDP_INVALID_ARGUMENT;
+  for (int l = 0; l < n_layers; ++l)
+    if (layers[l].d_in <= 0 || layers[l].d_out <= 0) return FLASHDP_INVALID_ARGUMENT;
+  const size_t inner = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, schedule);
+  if (inner == 0) return FLASHDP_UNSUPPORTED_SHAPE;
+  const size_t room = unpacked_bytes(layers, n_layers, B, T, dtype);
+  if (workspace && workspace_bytes < room + inner) return FLASHDP_WORKSPACE_TOO_SMALL;
+  int dev = 0;
+  int st = api::current_device(&dev);
+  if (st != FLASHDP_OK) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (!workspace) {
+    if ((st = api::library_workspace(room + inner, hs, &workspace)) != FLASHDP_OK) return st;
+    workspace_bytes = room + inner;
+  }
+  char* ws = static_cast<char*>(workspace);
+  // Layers in a row that share their activation (the projections of an attention block) are unpacked once and go to one call.
+  constexpr int RUN = 16;
+  for (int l = 0; l < n_layers;) {
+    flashdp_layer_t run[RUN];
+    int n = 0;
+    while (l + n < n_layers && n < RUN && layers[l + n].X == layers[l].X && layers[l + n].d_in == layers[l].d_in) {
+      run[n] = layers[l + n];
+      run[n].X = ws;
+      ++n;
+    }
+    st = flashdp_checkpoint8_unpack(layers[l].X, B * T, layers[l].d_in, dtype, ws, stream);
+    if (st == FLASHDP_OK)
+      st = flashdp_block_dp_grad_micro(run, n, B, T, dtype, schedule, ws + room, workspace_bytes - room, stream, accumulate, add_noise);
+    if (st != FLASHDP_OK) return st;
+    l += n;
+  }
+  return FLASHDP_OK;
+}
+
+}  // extern "C"

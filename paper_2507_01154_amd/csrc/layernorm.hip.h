@@ -1,0 +1,324 @@
+// Layer normalisation, forward and backward.
+//
+//   forward   mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), xh = (x - mu) r, y = xh gamma + beta
+//   backward  a = dy gamma, dx = r (a - mean(a) - xh mean(a xh));  per sample dgamma_i = sum_t dy xh, dbeta_i = sum_t dy
+//
+// Memory bound: 2 (backward: 3) values of the storage type an element.  A row is held in the registers of a wave (rows of up to 4 chunks of 16
+// bytes a lane) or of a workgroup and read once; the mean is known before deviations are squared, since sums of squares cancel
+// in a stream with an offset.  Backward, a thread holds the same columns of every row it meets, so the sums over tokens of dgamma and
+// dbeta stay in registers too: one workgroup goes through a chunk of a sample's tokens and leaves one partial sum
+// (vector_dp.hip.h adds them up).  Rows that no register file holds are read again for every sum.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "vector_io.hip.h"
+
+namespace flashdp {
+
+struct NormArgs {
+  const void* X;          // [rows][d]
+  const void* gamma;      // [d]
+  const void* beta;       // [d] or null
+  void* Y;
+  float* mean;            // [rows] or null
+  float* rstd;
+  int64_t rows, d;
+  float eps;
+};
+
+struct NormGradArgs {
+  const void* X;          // [B][T][d]
+  const void* dY;
+  const void* gamma;
+  const float* mean;      // [B * T]
+  const float* rstd;
+  void* dX;               // may be null, may be dY
+  float* partial;         // [B][chunks][2 d] (d without a bias); may be null
+  int64_t T, d;
+  int chunks, rows_per_chunk;
+  int bias;
+};
+
+// Sums of NV values over the workgroup of 4 waves, the same bits in every thread.  lds: 4 * NV floats that no thread still reads (two
+// buffers in turn need one barrier per sum).
+template <int NV>
+__device__ __forceinline__ void group_sum(float (&v)[NV], float* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) v[k] = wave_sum(v[k]);
+  if (lane == 0)
+#pragma unroll
+    for (int k = 0; k < NV; ++k) lds[k * 4 + wave] = v[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < NV; ++k) v[k] = (lds[k * 4] + lds[k * 4 + 1]) + (lds[k * 4 + 2] + lds[k * 4 + 3]);
+}
+
+// NT threads (64 or 256) share a row, CH chunks each.
+template <int DT, int NT, int CH>
+__global__ __launch_bounds__(256) void layernorm_forward_kernel(const NormArgs a) {
+  constexpr int N = Chunk<DT>::N;
+  __shared__ float lds[2][4];
+  const int t = threadIdx.x % NT;
+  const int64_t row = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT;
+  if (row >= a.rows) return;     // NT = 64: a whole wave, and there are no barriers; NT = 256: never
+  const char* x = (const char*)a.X + row * a.d * Chunk<DT>::BYTES;
+  u32x4_t raw[CH];
+  float s[1] = {0.0f};
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int64_t col = (int64_t)(c * NT + t) * N;
+    raw[c] = load_chunk<DT>(x, col, a.d - col);
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float f[N];
+    widen_chunk<DT>(raw[c], f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[0] += f[k];
+  }
+  if constexpr (NT == 64) s[0] = wave_sum(s[0]); else group_sum(s, lds[0]);
+  const float mu = s[0] / (float)a.d;
+  s[0] = 0.0f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int64_t left = a.d - (int64_t)(c * NT + t) * N;
+    float f[N];
+    widen_chunk<DT>(raw[c], f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float v = k < left ? f[k] - mu : 0.0f;
+      s[0] = fmaf(v, v, s[0]);
+    }
+  }
+  if constexpr (NT == 64) s[0] = wave_sum(s[0]); else group_sum(s, lds[1]);
+  const float r = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
+  char* y = (char*)a.Y + row * a.d * Chunk<DT>::BYTES;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
+    if (left > 0) {
+      float f[N], w[N], b[N];
+      widen_chunk<DT>(raw[c], f);
+      widen_chunk<DT>(load_chunk<DT>(a.gamma, col, left), w);
+      widen_chunk<DT>(a.beta ? load_chunk<DT>(a.beta, col, left) : u32x4_t{0u, 0u, 0u, 0u}, b);
+#pragma unroll
+      for (int k = 0; k < N; ++k) f[k] = fmaf((f[k] - mu) * r, w[k], b[k]);
+      store_chunk<DT>(y, col, left, round_chunk<DT>(f));
+    }
+  }
+  if (t == 0) {
+    if (a.mean) a.mean[row] = mu;
+    if (a.rstd) a.rstd[row] = r;
+  }
+}
+
+// Rows longer than the registers of a workgroup hold: one workgroup per row, read three times.
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_forward_long_kernel(const NormArgs a) {
+  constexpr int N = Chunk<DT>::N;
+  __shared__ float lds[2][4];
+  const int64_t row = blockIdx.x;
+  const char* x = (const char*)a.X + row * a.d * Chunk<DT>::BYTES;
+  float s[1] = {0.0f}, f[N];
+  for (int64_t col = (int64_t)threadIdx.x * N; col < a.d; col += 256 * N) {
+    widen_chunk<DT>(load_chunk<DT>(x, col, a.d - col), f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[0] += f[k];
+  }
+  group_sum(s, lds[0]);
+  const float mu = s[0] / (float)a.d;
+  s[0] = 0.0f;
+  for (int64_t col = (int64_t)threadIdx.x * N; col < a.d; col += 256 * N) {
+    widen_chunk<DT>(load_chunk<DT>(x, col, a.d - col), f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float v = k < a.d - col ? f[k] - mu : 0.0f;
+      s[0] = fmaf(v, v, s[0]);
+    }
+  }
+  group_sum(s, lds[1]);
+  const float r = 1.0f / sqrtf(s[0] / (float)a.d + a.eps);
+  char* y = (char*)a.Y + row * a.d * Chunk<DT>::BYTES;
+  for (int64_t col = (int64_t)threadIdx.x * N; col < a.d; col += 256 * N) {
+    float w[N], b[N];
+    widen_chunk<DT>(load_chunk<DT>(x, col, a.d - col), f);
+    widen_chunk<DT>(load_chunk<DT>(a.gamma, col, a.d - col), w);
+    widen_chunk<DT>(a.beta ? load_chunk<DT>(a.beta, col, a.d - col) : u32x4_t{0u, 0u, 0u, 0u}, b);
+#pragma unroll
+    for (int k = 0; k < N; ++k) f[k] = fmaf((f[k] - mu) * r, w[k], b[k]);
+    store_chunk<DT>(y, col, a.d - col, round_chunk<DT>(f));
+  }
+  if (threadIdx.x == 0) {
+    if (a.mean) a.mean[row] = mu;
+    if (a.rstd) a.rstd[row] = r;
+  }
+}
+
+__device__ __forceinline__ void store_sums4(float* to, int64_t col, int64_t left, const float* s) {
+  store_chunk<DT_F32>(to, col, left, u32x4_t{__builtin_bit_cast(uint32_t, s[0]), __builtin_bit_cast(uint32_t, s[1]),
+                                             __builtin_bit_cast(uint32_t, s[2]), __builtin_bit_cast(uint32_t, s[3])});
+}
+
+// One workgroup per (sample, chunk of tokens): its rows one after the other (NT = 256) or four waves' rows beside each other.
+template <int DT, int NT, int CH>
+__global__ __launch_bounds__(256) void layernorm_grad_kernel(const NormGradArgs a) {
+  constexpr int N = Chunk<DT>::N, ROWS = 256 / NT;
+  __shared__ float lds[NT == 64 ? 4 * 64 * N : 2 * 8];
+  const int t = threadIdx.x % NT;
+  const int64_t i = blockIdx.x / a.chunks, k0 = blockIdx.x - i * a.chunks;
+  const int64_t first = i * a.T + k0 * a.rows_per_chunk;
+  const int64_t last = (k0 + 1) * a.rows_per_chunk < a.T ? first + a.rows_per_chunk : (i + 1) * a.T;
+  const float per_d = 1.0f / (float)a.d;
+  u32x4_t w[CH];
+  float sg[CH][N], sb[CH][N];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int64_t col = (int64_t)(c * NT + t) * N;
+    w[c] = load_chunk<DT>(a.gamma, col, a.d - col);
+#pragma unroll
+    for (int k = 0; k < N; ++k) sg[c][k] = sb[c][k] = 0.0f;
+  }
+  int turn = 0;
+  for (int64_t row = first + threadIdx.x / NT; row < last; row += ROWS) {
+    const char* x = (const char*)a.X + row * a.d * Chunk<DT>::BYTES;
+    const char* dy = (const char*)a.dY + row * a.d * Chunk<DT>::BYTES;
+    u32x4_t xr[CH], gr[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int64_t col = (int64_t)(c * NT + t) * N;
+      xr[c] = load_chunk<DT>(x, col, a.d - col);
+      gr[c] = load_chunk<DT>(dy, col, a.d - col);
+    }
+    const float mu = a.mean[row], r = a.rstd[row];
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float f[N], g[N], v[N];
+      widen_chunk<DT>(xr[c], f);
+      widen_chunk<DT>(gr[c], g);
+      widen_chunk<DT>(w[c], v);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {     // (columns that do not exist have dy = gamma = 0)
+        const float xh = (f[k] - mu) * r, p = g[k] * v[k];
+        s[0] += p;
+        s[1] = fmaf(p, xh, s[1]);
+        sg[c][k] = fmaf(g[k], xh, sg[c][k]);
+        sb[c][k] += g[k];
+      }
+    }
+    if constexpr (NT == 64) { s[0] = wave_sum(s[0]); s[1] = wave_sum(s[1]); }
+    else { group_sum(s, lds + 8 * turn); turn ^= 1; }
+    if (a.dX) {
+      const float m0 = s[0] * per_d, m1 = s[1] * per_d;
+      char* dx = (char*)a.dX + row * a.d * Chunk<DT>::BYTES;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
+        if (left > 0) {
+          float f[N], g[N], v[N];
+          widen_chunk<DT>(xr[c], f);
+          widen_chunk<DT>(gr[c], g);
+          widen_chunk<DT>(w[c], v);
+#pragma unroll
+          for (int k = 0; k < N; ++k) f[k] = r * (fmaf(g[k], v[k], -m0) - (f[k] - mu) * r * m1);
+          store_chunk<DT>(dx, col, left, round_chunk<DT>(f));
+        }
+      }
+    }
+  }
+  if (!a.partial) return;
+  float* to = a.partial + (int64_t)blockIdx.x * a.d * (a.bias ? 2 : 1);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      if (part == 1 && !a.bias) break;
+      float* s = part ? sb[c] : sg[c];
+      if constexpr (NT == 64) {     // the four waves' sums, joined by the first
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) lds[k * 256 + threadIdx.x] = s[k];
+        __syncthreads();
+        if (threadIdx.x >= 64) continue;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          s[k] = (lds[k * 256 + t] + lds[k * 256 + 64 + t]) + (lds[k * 256 + 128 + t] + lds[k * 256 + 192 + t]);
+      }
+      if (left > 0)
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q) store_sums4(to + part * a.d, col + 4 * q, left - 4 * q, s + 4 * q);
+    }
+  }
+}
+
+// Rows longer than the registers of a workgroup hold.  First the sums over tokens, a thread per chunk of columns down the tokens of its
+// workgroup's chunk ...
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_grad_long_sums_kernel(const NormGradArgs a, int col_tiles) {
+  constexpr int N = Chunk<DT>::N;
+  const int64_t unit = blockIdx.x / col_tiles;
+  const int64_t col = ((int64_t)(blockIdx.x - unit * col_tiles) * 256 + threadIdx.x) * N, left = a.d - col;
+  if (left <= 0) return;
+  const int64_t i = unit / a.chunks, k0 = unit - i * a.chunks;
+  const int64_t first = i * a.T + k0 * a.rows_per_chunk;
+  const int64_t last = (k0 + 1) * a.rows_per_chunk < a.T ? first + a.rows_per_chunk : (i + 1) * a.T;
+  float sg[N], sb[N], f[N], g[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) sg[k] = sb[k] = 0.0f;
+#pragma unroll 2
+  for (int64_t row = first; row < last; ++row) {
+    widen_chunk<DT>(load_chunk<DT>((const char*)a.X + row * a.d * Chunk<DT>::BYTES, col, left), f);
+    widen_chunk<DT>(load_chunk<DT>((const char*)a.dY + row * a.d * Chunk<DT>::BYTES, col, left), g);
+    const float mu = a.mean[row], r = a.rstd[row];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      sg[k] = fmaf(g[k], (f[k] - mu) * r, sg[k]);
+      sb[k] += g[k];
+    }
+  }
+  float* to = a.partial + unit * a.d * (a.bias ? 2 : 1);
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) {
+    store_sums4(to, col + 4 * q, left - 4 * q, sg + 4 * q);
+    if (a.bias) store_sums4(to + a.d, col + 4 * q, left - 4 * q, sb + 4 * q);
+  }
+}
+
+// ... then dX (which may be dY, so not before the sums), one workgroup per row, read twice.
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_grad_long_rows_kernel(const NormGradArgs a) {
+  constexpr int N = Chunk<DT>::N;
+  __shared__ float lds[8];
+  const int64_t row = blockIdx.x;
+  const char* x = (const char*)a.X + row * a.d * Chunk<DT>::BYTES;
+  const char* dy = (const char*)a.dY + row * a.d * Chunk<DT>::BYTES;
+  const float mu = a.mean[row], r = a.rstd[row], per_d = 1.0f / (float)a.d;
+  float s[2] = {0.0f, 0.0f}, f[N], g[N], v[N];
+  for (int64_t col = (int64_t)threadIdx.x * N; col < a.d; col += 256 * N) {
+    widen_chunk<DT>(load_chunk<DT>(x, col, a.d - col), f);
+    widen_chunk<DT>(load_chunk<DT>(dy, col, a.d - col), g);
+    widen_chunk<DT>(load_chunk<DT>(a.gamma, col, a.d - col), v);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float p = g[k] * v[k];
+      s[0] += p;
+      s[1] = fmaf(p, (f[k] - mu) * r, s[1]);
+    }
+  }
+  group_sum(s, lds);
+  const float m0 = s[0] * per_d, m1 = s[1] * per_d;
+  char* dx = (char*)a.dX + row * a.d * Chunk<DT>::BYTES;
+  for (int64_t col = (int64_t)threadIdx.x * N; col < a.d; col += 256 * N) {
+    widen_chunk<DT>(load_chunk<DT>(x, col, a.d - col), f);
+    widen_chunk<DT>(load_chunk<DT>(dy, col, a.d - col), g);
+    widen_chunk<DT>(load_chunk<DT>(a.gamma, col, a.d - col), v);
+#pragma unroll
+    for (int k = 0; k < N; ++k) f[k] = r * (fmaf(g[k], v[k], -m0) - (f[k] - mu) * r * m1);
+    store_chunk<DT>(dx, col, a.d - col, round_chunk<DT>(f));
+  }
+}
+
+}  // namespace flashdp

@@ -169,9 +169,10 @@ FLASHDP_HD Normals4 box_muller4(const Words4& r) {
   return o;
 }
 
-// The four normals of group g (elements 4g .. 4g+3) of the field keyed by (seed, layer).
-FLASHDP_HD Normals4 noise_group(uint64_t seed, uint32_t layer, uint64_t g) {
-  return box_muller4(philox4x32_10((uint32_t)g, (uint32_t)(g >> 32), layer, 0u,
+// The four normals of group g (elements 4g .. 4g+3) of the field keyed by (seed, layer).  field, the last counter word, keeps
+// the parameters of one layer apart that share a seed: 0 for its weight, 1 for a bias, 2 for the parameters of a normalisation.
+FLASHDP_HD Normals4 noise_group(uint64_t seed, uint32_t layer, uint64_t g, uint32_t field = 0u) {
+  return box_muller4(philox4x32_10((uint32_t)g, (uint32_t)(g >> 32), layer, field,
                                    (uint32_t)seed, (uint32_t)(seed >> 32)));
 }
 
