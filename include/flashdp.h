@@ -61,6 +61,9 @@
  *                                256x256 with 32-deep k-tiles - these three stage tiles through registers -,
  *                                256x256, 384x192, 192x384 with 32-deep k-tiles loaded straight into LDS);
  *                                -1 sends fp32 inputs and sizes that are no multiples of 8 to the generic kernel;
+ *   FLASHDP_FORWARD = 0 .. 9     forces the kernel of flashdp_linear_forward where the shape allows it: direct-to-LDS tiles of 16 x 16, 16 x 32,
+ *                                32 x 32, 64 x 64, 128 x 128, 128 x 128 with two workgroups per CU, 256 x 256 (0 .. 6, d_in * size a
+ *                                multiple of 16 bytes); few rows, 64 x 64 and 128 x 128 tiles through registers (7 .. 9, other d_in);
  *   FLASHDP_OVERLAP_GRID = n     workgroups of the aggregation kernel in the overlapped schedule (default: one per
  *                                compute unit).
  */

@@ -13,6 +13,7 @@ __attribute__((visibility("hidden"))) int current_device(int* dev);
 // being captured, where FLASHDP_WORKSPACE_TOO_SMALL is the answer instead.
 __attribute__((visibility("hidden"))) int library_workspace(size_t need, hipStream_t stream, void** ptr);
 __attribute__((visibility("hidden"))) int64_t compute_units();
+__attribute__((visibility("hidden"))) int forward_override();   // FLASHDP_FORWARD, or -1
 __attribute__((visibility("hidden"))) void note_kernel(const char* name);
 __attribute__((visibility("hidden"))) hipError_t allow_lds(const void* kernel, int bytes);
 

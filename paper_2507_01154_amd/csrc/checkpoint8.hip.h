@@ -65,6 +65,24 @@ __device__ __forceinline__ void load_q(const signed char* q, int64_t left, uint3
   }
 }
 
+// The q of N values of scale 2^e = 1 / inv to q[0 ..], `left` of which exist.
+template <int N>
+__device__ __forceinline__ void store_q(signed char* q, int64_t left, const float (&f)[N], float inv) {
+  uint32_t v[N / 4];
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k)
+    v[k] = checkpoint8_quantise(f[4 * k], inv) | checkpoint8_quantise(f[4 * k + 1], inv) << 8 |
+           checkpoint8_quantise(f[4 * k + 2], inv) << 16 | checkpoint8_quantise(f[4 * k + 3], inv) << 24;
+  if (left >= N) {
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) ((u32_any_t*)q)[k] = v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < N - 1; ++k)
+      if (k < left) q[k] = (signed char)(v[k >> 2] >> (8 * (k & 3)));
+  }
+}
+
 // One thread per chunk of 16 bytes of x; the chunks of a row fill whole blocks (chunks past the row's end hold zeros and store
 // nothing), so the lanes of a block are neighbours in one wave.
 template <int DT>
@@ -84,21 +102,7 @@ __global__ __launch_bounds__(256) void checkpoint8_pack_kernel(const void* x, in
   for (int off = 1; off < PER; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
   if (left <= 0) return;
   const int e = checkpoint8_exponent<DT>(m);
-  const float inv = power_of_two(-e);
-  uint32_t v[N / 4];
-#pragma unroll
-  for (int k = 0; k < N / 4; ++k)
-    v[k] = checkpoint8_quantise(f[4 * k], inv) | checkpoint8_quantise(f[4 * k + 1], inv) << 8 |
-           checkpoint8_quantise(f[4 * k + 2], inv) << 16 | checkpoint8_quantise(f[4 * k + 3], inv) << 24;
-  signed char* to = q + row * d + col;
-  if (left >= N) {
-#pragma unroll
-    for (int k = 0; k < N / 4; ++k) ((u32_any_t*)to)[k] = v[k];
-  } else {
-#pragma unroll
-    for (int k = 0; k < N - 1; ++k)
-      if (k < left) to[k] = (signed char)(v[k >> 2] >> (8 * (k & 3)));
-  }
+  store_q<N>(q + row * d + col, left, f, power_of_two(-e));
   if (c % PER == 0) scales[block] = (unsigned char)(e + 127);
 }
 

@@ -116,7 +116,7 @@ struct Plan {
 // Environment overrides (measurement aids).  Read once per process, at the first call that needs them; with
 // FLASHDP_DEBUG_ENV=1 in the environment at that moment they are read again at every call instead (the test
 // suite switches kernels and schedules between calls this way).
-struct EnvOverrides { int tile = 0; int overlap_grid = 0; int schedule = -1; };
+struct EnvOverrides { int tile = 0; int overlap_grid = 0; int schedule = -1; int forward = -1; };
 
 int parse_schedule_name(const char* s) {
   if (!s || !*s) return -1;
@@ -136,6 +136,8 @@ EnvOverrides read_env() {
   s = std::getenv("FLASHDP_OVERLAP_GRID");
   if (s && *s) e.overlap_grid = std::atoi(s);
   e.schedule = parse_schedule_name(std::getenv("FLASHDP_SCHEDULE"));
+  s = std::getenv("FLASHDP_FORWARD");
+  if (s && *s) e.forward = std::atoi(s);
   return e;
 }
 
@@ -1127,6 +1129,7 @@ int library_workspace(size_t need, hipStream_t stream, void** ptr) {
   return st != FLASHDP_OK ? st : got < need ? FLASHDP_WORKSPACE_TOO_SMALL : FLASHDP_OK;
 }
 int64_t compute_units() { return plan_cus(); }
+int forward_override() { return env().forward; }
 void note_kernel(const char* name) { g_ctx.last_kernel = name; }
 hipError_t allow_lds(const void* kernel, int bytes) { return ensure_lds_limit(kernel, bytes); }
 

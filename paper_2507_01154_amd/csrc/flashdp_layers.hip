@@ -11,6 +11,9 @@
 #include "activation_dp.hip.h"
 #include "api_internal.h"
 #include "checkpoint8.hip.h"
+#include "forward_deep.hip.h"
+#include "forward_large.hip.h"
+#include "forward_rows.hip.h"
 #include "forward_tile.hip.h"
 #include "layernorm.hip.h"
 #include "vector_dp.hip.h"
@@ -157,16 +160,101 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   return p;
 }
 
-using Tile128x128 = ForwardTileCfg<128, 128>;
-using Tile64x64 = ForwardTileCfg<64, 64>;
+// ---- the forward product ----------------------------------------------------------------------------
 
+// Which kernel forms a product.  For rows of whole 16-byte chunks a ladder of tiles; a call takes the one whose rounds are
+// the shortest.  A round of `per_cu` workgroups on every compute unit takes start + tile * (k-tiles of 128 bytes) microseconds, one
+// of at most one workgroup per unit start + alone * k-tiles (fitted to 150 products of one to 8192 rows, 768 to 13824 features; 16-bit types,
+// then fp32, whose k-tiles are half as deep and bound by the matrix cores from 64 x 64 on).  us, in the order of the ladder (- = not tried):
+// bf16 1 x 4096 -> 4096: 7.2, 10.0, 10.0, 14.7, 34, -, -; fp16 8 x 768 -> 50257: 23.3, 16.6, 18.4, 22.4, -, -, -; bf16 128 x 4096 -> 4096: -, -, 14.6, 15.2, 34.9, 46, 74;
+// 256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
+// bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; fp32 128 x 4096 -> 4096: -, -, 45, 74, 257, 247, -; 2048 x 4096 -> 4096: -, -, 665, 588, 520, 480, 931.
+// Rows that no 16-byte chunks divide: direct loads to LDS need 4-byte alignment; few rows take the kernel that reads W straight into
+// registers, others tiles staged through registers (bf16 64 x 4096 -> 4096: 23.8, 39.5).
+enum ForwardPath { FWD_16x16 = 0, FWD_16x32, FWD_32x32, FWD_64x64, FWD_128x128, FWD_128x128_TWO, FWD_256x256, FWD_LADDER, FWD_ROWS = FWD_LADDER, FWD_ANY_64, FWD_ANY_128, FWD_PATHS };
+struct ForwardRung { int bm, bn, per_cu; double start, tile, alone, tile32, alone32; };   // tile32 = 0: not for fp32
+constexpr ForwardRung FORWARD_LADDER[FWD_LADDER] = {
+    {16, 16, 2, 1.9, 0.115, 0.085, 0.115, 0.09}, {16, 32, 3, 2.0, 0.15, 0.12, 0.3, 0.21}, {32, 32, 2, 1.6, 0.18, 0.1, 0.34, 0.2}, {64, 64, 1, 2.6, 0.19, 0.19, 0.56, 0.56},
+    {128, 128, 1, 4.0, 0.54, 0.54, 0.0, 0.0},    {128, 128, 2, 6.6, 0.87, 0.65, 3.7, 1.92},   {256, 256, 1, 7.0, 1.54, 1.54, 0.0, 0.0}};
+
+bool forward_direct(int64_t d_in, int dtype) {
+  const int64_t kb = d_in * (dtype == FLASHDP_F32 ? 4 : 2);
+  return kb % 16 == 0 && kb < (int64_t(1) << 23) - 4096;      // 256 rows lie within the 2 GiB that a buffer descriptor reaches
+}
+// tiles of a rung, or -1 where they are too many for a grid
+int64_t forward_tiles(int64_t rows, int64_t d_out, int bm, int bn) {
+  const int64_t tm = (rows + bm - 1) / bm, tn = (d_out + bn - 1) / bn;
+  return tm * 8 > GRID_LIMIT || tn * 8 > GRID_LIMIT || tm * tn > GRID_LIMIT ? -1 : tm * tn;
+}
+
+ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, bool blocks_of_32) {
+  const int forced = api::forward_override();
+  if (!forward_direct(d_in, dtype)) {
+    if (forced == FWD_ROWS || forced == FWD_ANY_64 || forced == FWD_ANY_128) return forced == FWD_ROWS && rows > 64 ? FWD_ANY_64 : (ForwardPath)forced;
+    return rows <= 64 ? FWD_ROWS : forward_tiles(rows, d_out, 128, 128) < 256 && forward_tiles(rows, d_out, 64, 64) >= 0 ? FWD_ANY_64 : FWD_ANY_128;
+  }
+  const int64_t cus = api::compute_units(), nk = (d_in * (dtype == FLASHDP_F32 ? 4 : 2) + 127) / 128;
+  int best = -1;
+  double least = 0.0;
+  for (int r = 0; r < FWD_LADDER; ++r) {
+    const ForwardRung& g = FORWARD_LADDER[r];
+    if ((blocks_of_32 && g.bn % CKPT8_BLOCK != 0) || (dtype == FLASHDP_F32 && g.tile32 == 0.0)) continue;
+    const int64_t tiles = forward_tiles(rows, d_out, g.bm, g.bn);
+    if (tiles < 0) continue;
+    if (forced == r) return (ForwardPath)r;
+    const int64_t slots = cus * g.per_cu, rest = tiles % slots;
+    const double tile = dtype == FLASHDP_F32 ? g.tile32 : g.tile, alone = dtype == FLASHDP_F32 ? g.alone32 : g.alone;
+    const double t = (double)(tiles / slots) * (g.start + tile * nk) + (rest == 0 ? 0.0 : g.start + (rest <= cus ? alone : tile) * nk);
+    if (best < 0 || t < least) { best = r; least = t; }
+  }
+  return best < 0 ? FWD_PATHS : (ForwardPath)best;
+}
+
+template <typename Cfg>
+hipError_t launch_forward(void (*kernel)(ForwardArgs), ForwardArgs& a, int64_t grid, hipStream_t st) {
+  const hipError_t e = api::allow_lds(reinterpret_cast<const void*>(kernel), Cfg::LDS_BYTES);
+  return e != hipSuccess ? e : launch(kernel, grid, Cfg::NT, Cfg::LDS_BYTES, st, a);
+}
+template <typename Cfg>
+hipError_t launch_forward_tiles(void (*kernel)(ForwardArgs), ForwardArgs& a, hipStream_t st) {
+  a.tiles_m = (int)((a.rows + Cfg::BM - 1) / Cfg::BM);
+  a.tiles_n = (int)(((int64_t)a.D + Cfg::BN - 1) / Cfg::BN);
+  return launch_forward<Cfg>(kernel, a, (int64_t)a.tiles_m * a.tiles_n, st);
+}
 template <typename Cfg, int DT>
-hipError_t launch_forward_tile(ForwardArgs& a, hipStream_t st) {
-  const int64_t tm = (a.rows + Cfg::BM - 1) / Cfg::BM, tn = ((int64_t)a.D + Cfg::BN - 1) / Cfg::BN;
-  if (tm * 8 > GRID_LIMIT || tn * 8 > GRID_LIMIT || tm * tn > GRID_LIMIT) return hipErrorInvalidValue;
-  a.tiles_m = (int)tm; a.tiles_n = (int)tn;
-  const hipError_t e = api::allow_lds(reinterpret_cast<const void*>(forward_tile_kernel<Cfg, DT>), Cfg::LDS_BYTES);
-  return e != hipSuccess ? e : launch(forward_tile_kernel<Cfg, DT>, tm * tn, Cfg::NT, Cfg::LDS_BYTES, st, a);
+hipError_t launch_forward_rows(ForwardArgs& a, hipStream_t st) {
+  return launch_forward<Cfg>(forward_rows_kernel<Cfg, DT>, a, ((int64_t)a.D + 16 * Cfg::NF - 1) / (16 * Cfg::NF), st);
+}
+
+using Deep16x16 = ForwardDeepCfg<16, 16, 4, 1, 16, 4>;
+using Deep16x32 = ForwardDeepCfg<16, 32, 2, 1, 8, 2>;
+using Deep32x32 = ForwardDeepCfg<32, 32, 4, 1, 8, 2>;
+using Deep64x64 = ForwardDeepCfg<64, 64, 4, 2, 8, 2>;
+using Deep128x128 = ForwardDeepCfg<128, 128, 2, 4, 4, 1>;
+
+template <int DT>
+hipError_t run_forward(ForwardPath path, ForwardArgs& a, hipStream_t st) {
+  switch (path) {
+    case FWD_16x16: return launch_forward_tiles<Deep16x16>(forward_deep_kernel<Deep16x16, DT>, a, st);
+    case FWD_16x32: return launch_forward_tiles<Deep16x32>(forward_deep_kernel<Deep16x32, DT>, a, st);
+    case FWD_32x32: return launch_forward_tiles<Deep32x32>(forward_deep_kernel<Deep32x32, DT>, a, st);
+    case FWD_64x64: return launch_forward_tiles<Deep64x64>(forward_deep_kernel<Deep64x64, DT>, a, st);
+    case FWD_128x128: if constexpr (DT != DT_F32) return launch_forward_tiles<Deep128x128>(forward_deep_kernel<Deep128x128, DT>, a, st); else return hipErrorInvalidValue;
+    case FWD_128x128_TWO: return launch_forward_tiles<ForwardLarge128>(forward_large_kernel<ForwardLarge128, DT>, a, st);
+    case FWD_256x256: if constexpr (DT != DT_F32) return launch_forward_tiles<ForwardLarge256>(forward_large_kernel<ForwardLarge256, DT>, a, st); else return hipErrorInvalidValue;
+    case FWD_ROWS:
+      if (a.rows <= 16) return launch_forward_rows<ForwardRowsCfg<2, 1, 8>, DT>(a, st);
+      if (a.rows <= 32) return launch_forward_rows<ForwardRowsCfg<2, 2, 8>, DT>(a, st);
+      return launch_forward_rows<ForwardRowsCfg<2, 4, 8>, DT>(a, st);
+    case FWD_ANY_64: return launch_forward_tiles<ForwardTileCfg<64, 64>>(forward_tile_kernel<ForwardTileCfg<64, 64>, DT>, a, st);
+    case FWD_ANY_128: return launch_forward_tiles<ForwardTileCfg<128, 128>>(forward_tile_kernel<ForwardTileCfg<128, 128>, DT>, a, st);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+const char* forward_kernel_name(ForwardPath path) {
+  return path == FWD_ROWS ? "forward_rows_kernel" : path == FWD_ANY_64 || path == FWD_ANY_128 ? "forward_tile_kernel"
+         : path == FWD_128x128_TWO || path == FWD_256x256 ? "forward_large_kernel" : "forward_deep_kernel";
 }
 
 }  // namespace
@@ -179,8 +267,9 @@ int flashdp_linear_forward(const void* X, const void* W, const void* bias, const
   int st = check_rows(rows, d_in);
   if (st == FLASHDP_OK) st = check_rows(rows, d_out);
   if (st != FLASHDP_OK) return st;
-  // (grid of the smallest tiles)
-  if ((rows + 63) / 64 * 8 > GRID_LIMIT || (rows + 63) / 64 * ((d_out + 63) / 64) > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  const ForwardPath path = forward_path(rows, d_in, d_out, dtype, z_8bit != 0);
+  if (path == FWD_PATHS || (path >= FWD_ANY_64 && forward_tiles(rows, d_out, path == FWD_ANY_64 ? 64 : 128, path == FWD_ANY_64 ? 64 : 128) < 0))
+    return FLASHDP_UNSUPPORTED_SHAPE;    // more tiles than a grid holds
   if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(Z, 16)) return FLASHDP_MISALIGNED;
   int dev = 0;
   if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
@@ -191,12 +280,8 @@ int flashdp_linear_forward(const void* X, const void* W, const void* bias, const
   a.act = activation; a.keep = !Z ? KEEP_NONE : z_8bit ? KEEP_EIGHT : KEEP_SAME;
   a.tiles_m = a.tiles_n = 0;
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  const bool large = ((rows + 127) / 128) * ((d_out + 127) / 128) >= 256;
-  HIP_TRY(by_dtype(dtype, [&](auto dt) {
-    constexpr int DT = decltype(dt)::value;
-    return large ? launch_forward_tile<Tile128x128, DT>(a, hs) : launch_forward_tile<Tile64x64, DT>(a, hs);
-  }));
-  api::note_kernel("forward_tile_kernel");
+  HIP_TRY(by_dtype(dtype, [&](auto dt) { return run_forward<decltype(dt)::value>(path, a, hs); }));
+  api::note_kernel(forward_kernel_name(path));
   return FLASHDP_OK;
 }
 

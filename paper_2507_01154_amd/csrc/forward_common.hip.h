@@ -6,8 +6,7 @@
 // both operands in step s.  So all kernels see rows of bytes: a k-step is 64 bytes of every row, whatever the type.
 //
 // W is the first operand and X the second: register r of lane l is then feature 4 (l / 16) + r of token l % 16, four
-// consecutive features that leave in one store, and a block of 32 features that shares an 8-bit exponent is two registers' worth in the
-// four lanes l, l + 16, l + 32, l + 48.
+// consecutive features of one token.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -52,128 +51,123 @@ __device__ __forceinline__ f32x4v_t k_step(const u32x4_t w, const u32x4_t x, f32
   }
 }
 
-__device__ __forceinline__ float act_of(int act, float z) {
+template <int N>
+__device__ __forceinline__ void act_chunk(int act, const float (&z)[N], float (&y)[N]) {
+  auto each = [&](auto act_c) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) y[k] = act_value<decltype(act_c)::value>(z[k]);
+  };
   switch (act) {
-    case ACT_RELU: return act_value<ACT_RELU>(z);
-    case ACT_GELU: return act_value<ACT_GELU>(z);
-    case ACT_GELU_TANH: return act_value<ACT_GELU_TANH>(z);
-    case ACT_SILU: return act_value<ACT_SILU>(z);
-    default: return z;
+    case ACT_RELU: each(std::integral_constant<int, ACT_RELU>{}); break;
+    case ACT_GELU: each(std::integral_constant<int, ACT_GELU>{}); break;
+    case ACT_GELU_TANH: each(std::integral_constant<int, ACT_GELU_TANH>{}); break;
+    case ACT_SILU: each(std::integral_constant<int, ACT_SILU>{}); break;
+    default: each(std::integral_constant<int, ACT_NONE>{}); break;
   }
 }
 
-// Four consecutive elements from index `at` on (any alignment), `left` of which exist.
-typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
+// The 8-bit form of a chunk of token m, `left` of its features from col on existing (none: the lane only takes part); the lanes
+// of a block of 32 features are neighbours, all of the same token.
 template <int DT>
-__device__ __forceinline__ void load4(const void* p, int64_t at, int left, float (&f)[4]) {
-  if constexpr (DT == DT_F32) {
-    const u32x4_t v = load_chunk<DT_F32>(p, at, left);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = as_float(v[k]);
-  } else {
-    uint32_t v[2] = {0u, 0u};
-    if (left >= 4) {
-      const u32x2_any_t q = *(const u32x2_any_t*)((const unsigned short*)p + at);
-      v[0] = q[0]; v[1] = q[1];
-    } else {
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (k < left) v[k >> 1] |= (uint32_t)((const unsigned short*)p)[at + k] << (16 * (k & 1));
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t h = (v[k >> 1] >> (16 * (k & 1))) & 0xFFFFu;
-      f[k] = DT == DT_BF16 ? __builtin_bit_cast(float, h << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)h);
-    }
-  }
-}
-template <int DT>
-__device__ __forceinline__ void store4(void* p, int64_t at, int left, const float (&f)[4]) {
-  if constexpr (DT == DT_F32) {
-    store_chunk<DT_F32>(p, at, left, u32x4_t{__builtin_bit_cast(uint32_t, f[0]), __builtin_bit_cast(uint32_t, f[1]),
-                                             __builtin_bit_cast(uint32_t, f[2]), __builtin_bit_cast(uint32_t, f[3])});
-  } else {
-    const u32x2_any_t q = {pack2_16bit<DT>(f[0], f[1]), pack2_16bit<DT>(f[2], f[3])};
-    if (left >= 4) {
-      *(u32x2_any_t*)((unsigned short*)p + at) = q;
-    } else {
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (k < left) ((unsigned short*)p)[at + k] = (unsigned short)(q[k >> 1] >> (16 * (k & 1)));
-    }
-  }
-}
-
-// The 8-bit form of a block of 32 features of token m that the lanes l, l + 16, l + 32, l + 48 hold: z[0] are features n .. n + 3 and
-// z[1] n + 16 .. n + 19, n = the block's first + 4 (lane / 16).  ok: the token exists (all lanes take part all the same).
-template <int DT>
-__device__ __forceinline__ void keep_block8(const ForwardArgs& a, int64_t m, int n, bool ok, const float (&z)[2][4]) {
+__device__ __forceinline__ void keep_chunk8(const ForwardArgs& a, int64_t m, int64_t col, int64_t left, const float (&z)[Chunk<DT>::N]) {
+  constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;
   float top = 0.0f;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int k = 0; k < N; ++k) top = fmaxf(top, k < left && finite_f32(z[k]) ? fabsf(z[k]) : 0.0f);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_f32(z[h][k]) && n + 16 * h + k < a.D ? fabsf(z[h][k]) : 0.0f);
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
-  if (!ok) return;
+  for (int off = 1; off < PER; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+  if (left <= 0) return;
   const int e = checkpoint8_exponent<DT>(top);
-  const float inv = power_of_two(-e);
-  signed char* row = (signed char*)a.Z + m * a.D;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = n + 16 * h;
-    uint32_t q = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) q |= checkpoint8_quantise(z[h][k], inv) << (8 * k);
-    if (a.D - col >= 4) {
-      *(u32_any_t*)(row + col) = q;
-    } else {
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (col + k < a.D) row[col + k] = (signed char)(q >> (8 * k));
-    }
-  }
-  if ((threadIdx.x & 63) < 16 && n < a.D) a.scales[m * checkpoint8_blocks(a.D) + n / CKPT8_BLOCK] = (unsigned char)(e + 127);
+  store_q<N>((signed char*)a.Z + m * a.D + col, left, z, power_of_two(-e));
+  if (col % CKPT8_BLOCK == 0) a.scales[m * checkpoint8_blocks(a.D) + col / CKPT8_BLOCK] = (unsigned char)(e + 127);
 }
 
-// What happens to finished sums: acc[i][j] is the 16 x 16 block of tokens m0 + 16 i .. and features n0 + 16 j .. of this wave
-// (n0 a multiple of 32).  Straight from the registers to memory.
+// What becomes of a chunk of sums Z of token m, features from col on, `left` of which exist (none: the lane only takes part).
+template <int DT>
+__device__ __forceinline__ void finish_chunk(const ForwardArgs& a, int64_t m, int64_t col, int64_t left, const float (&z)[Chunk<DT>::N]) {
+  constexpr int N = Chunk<DT>::N;
+  const int64_t row = m * a.D * Chunk<DT>::BYTES;
+  u32x4_t res = {0u, 0u, 0u, 0u};
+  if (a.residual && left > 0) res = load_chunk<DT>((const char*)a.residual + row, col, left);
+  if (a.keep == KEEP_EIGHT) keep_chunk8<DT>(a, m, col, left, z);
+  if (left <= 0) return;
+  if (a.keep == KEEP_SAME) store_chunk<DT>((char*)a.Z + row, col, left, round_chunk<DT>(z));
+  float y[N];
+  act_chunk<N>(a.act, z, y);
+  if (a.residual) {
+    float w[N];
+    widen_chunk<DT>(res, w);
+#pragma unroll
+    for (int k = 0; k < N; ++k) y[k] += w[k];
+  }
+  store_chunk<DT>((char*)a.Y + row, col, left, round_chunk<DT>(y));
+}
+
+// The end of kernels whose waves share out the k-steps: PARTS partial sums of M tokens x F features in LDS (rows of F + 4 floats) are joined in
+// order, one chunk per thread and step.  Whole waves stay together (lanes of a block of 32 features exchange its largest magnitude).
+template <int DT, int NT, int PARTS, int M, int F>
+__device__ __forceinline__ void finish_partials(const ForwardArgs& a, const float* part, int64_t m0, int n0) {
+  constexpr int N = Chunk<DT>::N, PITCH = F + 4, PER_ROW = F / N, CHUNKS = M * PER_ROW;
+  for (int e = threadIdx.x; e < (CHUNKS + 63) / 64 * 64; e += NT) {
+    const int r = CHUNKS % 64 == 0 ? e / PER_ROW : min(e / PER_ROW, M - 1), c = (e % PER_ROW) * N;
+    const int64_t m = m0 + r, col = n0 + c, left = e < CHUNKS && m < a.rows ? a.D - col : 0;
+    float z[N];
+    widen_chunk<DT>(a.bias ? load_chunk<DT>(a.bias, col, left) : u32x4_t{0u, 0u, 0u, 0u}, z);
+#pragma unroll
+    for (int k = 0; k < N; k += 4) {
+      f32x4v_t sum = *(const f32x4v_t*)(part + r * PITCH + c + k);
+#pragma unroll
+      for (int v = 1; v < PARTS; ++v) sum += *(const f32x4v_t*)(part + (v * M + r) * PITCH + c + k);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) z[k + q] += sum[q];
+    }
+    finish_chunk<DT>(a, m, col, left, z);
+  }
+}
+
+// What happens to finished sums.  acc[i][j] is the 16 x 16 block of tokens m0 + 16 i .. and features n0 + 16 j .. of this wave (n0 a
+// multiple of 32).  They pass through `stage`, LDS of this wave alone, 64 tokens at a time, and leave as whole rows of chunks of 16 bytes: full
+// cache lines, one chunk per lane and step, so that the code of the epilogue exists once and not once per block.  Rows of the stage are
+// 16 bytes longer than their values, which spreads the 16 tokens that a store of sums meets over all banks.
+template <int FM, int FN>
+struct ForwardStage {
+  static constexpr int FEATURES = 16 * FN, BLOCKS = FM < 4 ? FM : 4, PITCH = FEATURES + 4;   // floats
+  static constexpr int BYTES = 16 * BLOCKS * PITCH * 4;                                     // per wave
+};
+
 template <int DT, int FM, int FN>
-__device__ __forceinline__ void forward_epilogue(const ForwardArgs& a, f32x4v_t (&acc)[FM][FN], int64_t m0, int n0) {
-  static_assert(FN % 2 == 0, "blocks of 32 features");
+__device__ __forceinline__ void forward_epilogue(const ForwardArgs& a, const f32x4v_t (&acc)[FM][FN], int64_t m0, int n0, float* stage) {
+  using S = ForwardStage<FM, FN>;
+  constexpr int N = Chunk<DT>::N, PER_ROW = S::FEATURES / N, ROWS = 64 / PER_ROW;
+  static_assert(FM % S::BLOCKS == 0 && S::FEATURES % CKPT8_BLOCK == 0, "whole phases, whole blocks of 32 features");
   const int lane = threadIdx.x & 63;
+  const int c = (lane % PER_ROW) * N, r0 = lane / PER_ROW;
+  const int64_t col = n0 + c, left = a.D - col;
+  float b[N];
+  widen_chunk<DT>(a.bias ? load_chunk<DT>(a.bias, col, left) : u32x4_t{0u, 0u, 0u, 0u}, b);
 #pragma unroll
-  for (int j = 0; j < FN; j += 2) {
-    const int n = n0 + 16 * j + 4 * (lane >> 4);
-    float b[2][4];
+  for (int phase = 0; phase < FM / S::BLOCKS; ++phase) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int i = 0; i < S::BLOCKS; ++i)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) b[h][k] = 0.0f;
-      if (a.bias) load4<DT>(a.bias, n + 16 * h, a.D - n - 16 * h, b[h]);
-    }
+      for (int j = 0; j < FN; ++j)
+        *(f32x4v_t*)(stage + (16 * i + (lane & 15)) * S::PITCH + 16 * j + 4 * (lane >> 4)) = acc[phase * S::BLOCKS + i][j];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+    for (int it = 0; it < 16 * S::BLOCKS / ROWS; ++it) {
+      const int r = it * ROWS + r0;
+      const int64_t m = m0 + 16 * S::BLOCKS * phase + r;
+      const bool ok = m < a.rows && left > 0;
+      float z[N];
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int64_t m = m0 + 16 * i + (lane & 15);
-      const bool ok = m < a.rows;
-      float z[2][4];
+      for (int k = 0; k < N; k += 4) {
+        const f32x4v_t s = *(const f32x4v_t*)(stage + r * S::PITCH + c + k);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) z[h][k] = acc[i][j + h][k] + b[h][k];
-      if (a.keep == KEEP_EIGHT) keep_block8<DT>(a, m, n, ok, z);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int col = n + 16 * h, left = a.D - col;
-        if (!ok || left <= 0) continue;
-        if (a.keep == KEEP_SAME) store4<DT>(a.Z, m * a.D + col, left, z[h]);
-        float y[4], r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.residual) load4<DT>(a.residual, m * a.D + col, left, r);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = act_of(a.act, z[h][k]) + r[k];
-        store4<DT>(a.Y, m * a.D + col, left, y);
+        for (int e = 0; e < 4; ++e) z[k + e] = s[e] + b[k + e];
       }
+      finish_chunk<DT>(a, m, col, ok ? left : 0, z);
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 

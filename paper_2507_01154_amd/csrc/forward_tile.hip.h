@@ -1,4 +1,4 @@
-// The forward product on tiles of BM tokens x BN features, any sizes, any alignment of rows.
+// The forward product on tiles of BM tokens x BN features, for rows that may start anywhere (K no multiple of 16 bytes).
 //
 // Four waves, 2 x 2; k-tiles of 128 bytes a row go through registers (loads of any alignment, zeros beyond the ends) into one of two LDS
 // buffers, one barrier per k-tile.  Rows of LDS are 144 bytes apart, so that the 16 rows that a fragment read meets at one 16-byte column
@@ -17,6 +17,7 @@ struct ForwardTileCfg {
   static constexpr int CHUNKS = ROWS * 8 / NT;               // 16-byte chunks per thread and k-tile
   static constexpr int LDS_BYTES = 2 * ROWS * PITCH;
   static constexpr int FM = BM / 32, FN = BN / 32;           // 16 x 16 blocks per wave
+  static_assert(4 * ForwardStage<FM, FN>::BYTES <= LDS_BYTES, "the epilogue's stages lie in the operand buffers");
 };
 
 template <typename Cfg, int DT>
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(Cfg::NT) void forward_tile_kernel(const ForwardArgs
     if (kt + 1 < nk) put((kt + 1) & 1);      // the buffer that k-tile kt - 1 was read from, before the last barrier
     __syncthreads();
   }
-  forward_epilogue<DT, FM, FN>(a, acc, m0 + wm, n0 + wn);
+  forward_epilogue<DT, FM, FN>(a, acc, m0 + wm, n0 + wn, (float*)(tiles_lds + wave * ForwardStage<FM, FN>::BYTES));
 }
 
 }  // namespace flashdp

@@ -15,7 +15,7 @@ import torch
 
 import paper_2507_01154_amd as F
 from oracle import flashdp_oracle as O
-from gpu_util import DEV
+from gpu_util import DEV, env
 
 pytestmark = pytest.mark.gpu
 
@@ -158,6 +158,25 @@ def test_forward_epilogues(rows, act, dtype):
     for k, (bias, residual, keep) in enumerate([(False, True, None), (True, False, "dtype"), (True, True, "8bit"), (False, False, "8bit")]):
         check_forward(rows, 136, 200, dtype, act, bias, residual, keep, seed=20 + k)
     check_forward(rows, 136, 200, dtype, act, True, True, None, seed=30, inplace=True)      # added to the residual in place
+
+
+# the kernels of the ladder (0 to 6: rows of whole 16-byte chunks; 4 and 6 are not made for fp32) and those for other rows (7 to 9), on sizes that
+# leave them ragged edges, one k-tile and many, and more k-tiles than stages
+FORCED = [(k, r, K, D) for k in range(7) for r, K, D in [(1, 8, 8), (5, 64, 40), (33, 136, 72), (70, 1160, 136), (300, 520, 328)]] + \
+         [(k, r, K, D) for k in (7, 8, 9) for r, K, D in [(1, 1, 8), (5, 63, 40), (33, 137, 75), (64, 1161, 137), (150, 517, 329)]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "fp32"])
+@pytest.mark.parametrize("kernel,rows,K,D", FORCED)
+def test_every_forward_kernel(kernel, rows, K, D, dtype):
+    with env(FLASHDP_FORWARD=kernel):
+        check_forward(rows, K, D, dtype, "none", False, False, None, seed=40)
+        check_forward(rows, K, D, dtype, "gelu", True, True, "dtype", seed=50)
+        check_forward(rows, K, D, dtype, "silu", True, False, "8bit", seed=60)
+        want = {7: "forward_rows_kernel" if rows <= 64 else "forward_tile_kernel", 8: "forward_tile_kernel", 9: "forward_tile_kernel",
+                5: "forward_large_kernel", 6: "forward_large_kernel"}.get(kernel, "forward_deep_kernel")
+        if dtype != "fp32" or kernel not in (4, 6):
+            assert F.flashdp_last_kernel() == want or kernel == 0           # (8-bit blocks of 32 features are wider than the smallest tile)
 
 
 @pytest.mark.parametrize("rows,K,D,dtype", [(1024, 768, 2304, "bf16"), (777, 1096, 2312, "f16"), (520, 1001, 1003, "bf16"), (512, 768, 776, "fp32"), (1500, 515, 770, "fp32"),

@@ -29,7 +29,7 @@ FORWARD = dict(X=A, W=B_, bias=None, residual=None, rows=4, d_in=8, d_out=8, dty
     (dict(z_8bit=2, Z=D_), INV), (dict(z_8bit=1), INV), (dict(rows=0), INV), (dict(d_in=0), INV), (dict(d_out=-1), INV),
     (dict(X=A + 8), MIS), (dict(W=B_ + 2), MIS), (dict(bias=D_ + 4), MIS), (dict(residual=D_ + 8), MIS), (dict(Y=C_ + 1), MIS), (dict(Z=D_ + 8), MIS),
     (dict(rows=1 << 40), SHAPE), (dict(d_in=(1 << 30) + 1), SHAPE), (dict(d_out=(1 << 30) + 1), SHAPE), (dict(rows=1 << 38), SHAPE),
-    (dict(rows=1 << 22, d_out=1 << 22), SHAPE)])
+    (dict(rows=1 << 30, d_out=1 << 20), SHAPE), (dict(rows=1 << 30, d_in=9, d_out=1 << 20), SHAPE)])
 def test_forward_refuses(changes, want):
     refused("flashdp_linear_forward", FORWARD, changes, want)
 
