@@ -50,51 +50,55 @@ __global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs
 #pragma unroll
   for (int k = 0; k < N; ++k) sum[k] = 0.0f;
   if (left > 0) {
+    const int64_t at = (row0 + r) * a.d + col, step = (int64_t)rt * a.d;          // elements; from row to row of this thread
+    const char* dyp = (const char*)a.dY + at * Chunk<DT>::BYTES;
+    const char* zp = (const char*)a.Z + at * (ZK == Z_EIGHT ? 1 : Chunk<DT>::BYTES);
+    const unsigned char* sp = a.scales + (row0 + r) * nb + col / CKPT8_BLOCK;
+    char* dzp = (char*)a.dZ + at * Chunk<DT>::BYTES;
+    const int64_t step_b = step * Chunk<DT>::BYTES, step_z = ZK == Z_EIGHT ? step : step_b, step_s = rt * nb;
     for (int64_t row = row0 + r; row < row1; row += (int64_t)rt * UNROLL) {
       u32x4_t dy[UNROLL], zr[UNROLL];
       uint32_t zq[UNROLL][N / 4];
       int sc[UNROLL];
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u) {
-        const int64_t rw = row + (int64_t)u * rt;
-        if (rw < row1) {
-          dy[u] = load_chunk<DT>((const char*)a.dY + rw * a.d * Chunk<DT>::BYTES, col, left);
-          if constexpr (ZK == Z_SAME) zr[u] = load_chunk<DT>((const char*)a.Z + rw * a.d * Chunk<DT>::BYTES, col, left);
+        if (row + (int64_t)u * rt < row1) {
+          dy[u] = load_chunk<DT>(dyp + u * step_b, 0, left);
+          if constexpr (ZK == Z_SAME) zr[u] = load_chunk<DT>(zp + u * step_z, 0, left);
           if constexpr (ZK == Z_EIGHT) {
-            load_q<N>((const signed char*)a.Z + rw * a.d + col, left, zq[u]);
-            sc[u] = a.scales[rw * nb + col / CKPT8_BLOCK];
+            load_q<N>((const signed char*)zp + u * step_z, left, zq[u]);
+            sc[u] = sp[u * step_s];
           }
         }
       }
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u) {
-        const int64_t rw = row + (int64_t)u * rt;
-        if (rw < row1) {
+        if (row + (int64_t)u * rt < row1) {
           float f[N], z[N];
           widen_chunk<DT>(dy[u], f);
           if constexpr (ZK == Z_SAME) widen_chunk<DT>(zr[u], z);
-          if constexpr (ZK == Z_EIGHT) {
-            const float scale = power_of_two(sc[u] - 127);
-#pragma unroll
-            for (int k = 0; k < N; ++k) z[k] = checkpoint8_value(zq[u][k >> 2], k & 3, scale);
-          }
+          if constexpr (ZK == Z_EIGHT) checkpoint8_values<N>(zq[u], power_of_two(sc[u] - 127), z);
 #pragma unroll
           for (int k = 0; k < N; ++k) {
             if constexpr (ZK != Z_NONE) f[k] *= act_slope<ACT>(z[k]);
             sum[k] += f[k];
           }
-          if (a.dZ) store_chunk<DT>((char*)a.dZ + rw * a.d * Chunk<DT>::BYTES, col, left, round_chunk<DT>(f));
+          if (a.dZ) store_chunk<DT>(dzp + u * step_b, 0, left, round_chunk<DT>(f));
           if constexpr (TOKEN) {
             if (a.partial) {
 #pragma unroll
               for (int q = 0; q < N / 4; ++q)
-                store_chunk<DT_F32>(a.partial + rw * a.d, col + 4 * q, left - 4 * q,
+                store_chunk<DT_F32>(a.partial + at + u * step, 4 * q, left - 4 * q,
                                     u32x4_t{__builtin_bit_cast(uint32_t, f[4 * q]), __builtin_bit_cast(uint32_t, f[4 * q + 1]),
                                             __builtin_bit_cast(uint32_t, f[4 * q + 2]), __builtin_bit_cast(uint32_t, f[4 * q + 3])});
             }
           }
         }
       }
+      dyp += UNROLL * step_b;
+      zp += UNROLL * step_z;
+      sp += UNROLL * step_s;
+      dzp += UNROLL * step_b;
     }
   }
   if constexpr (!TOKEN) {

@@ -36,16 +36,58 @@ __device__ __forceinline__ int checkpoint8_exponent(float m) {
   const int e = (int)(__builtin_bit_cast(uint32_t, m) >> 23) - 127 - 6;
   return e < Checkpoint8Least<DT>::EXP ? Checkpoint8Least<DT>::EXP : e;
 }
-// q of x in a block of scale 2^-e = inv, in the low byte
-__device__ __forceinline__ uint32_t checkpoint8_quantise(float x, float inv) {
-  const float r = fminf(fmaxf(__builtin_rintf(x * inv), -127.0f), 127.0f);
-  const int q = (int)r;
-  return finite_f32(x) ? (uint32_t)q & 0xFFu : 0x80u;
+// The largest m of PER (4 or 8) neighbouring lanes, in all of them.
+template <int PER>
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t m) {
+  m = max(m, lane_exchange<LANE_XOR_1>(m));
+  m = max(m, lane_exchange<LANE_XOR_2>(m));
+  return PER == 8 ? max(m, lane_exchange<LANE_REVERSE_8>(m)) : m;
 }
-// the value of byte k (0..3) of four q, scale 2^e
-__device__ __forceinline__ float checkpoint8_value(uint32_t q4, int k, float scale) {
-  const int q = (int)(q4 << (24 - 8 * k)) >> 24;
-  return q == -128 ? __builtin_bit_cast(float, 0x7FC00000u) : (float)q * scale;
+
+// The largest finite magnitude of N values, agreed on by PER neighbouring lanes that hold a block; values from `left` on do not exist (zeros).
+// Magnitudes are compared as integers; only a block that has a value which is not finite is gone through again without it.
+template <int N, int PER>
+__device__ __forceinline__ float checkpoint8_top(const float (&f)[N]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = max(m, __builtin_bit_cast(uint32_t, f[k]) & 0x7FFFFFFFu);
+  m = max_of_lanes<PER>(m);
+  if (m >= 0x7F800000u) {     // the same in all lanes of the block
+    m = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) m = max(m, finite_f32(f[k]) ? __builtin_bit_cast(uint32_t, f[k]) & 0x7FFFFFFFu : 0u);
+    m = max_of_lanes<PER>(m);
+  }
+  return __builtin_bit_cast(float, m);
+}
+// Four q, a byte each, of values in a block of scale 2^-e = inv.  Cut to -127 .. 127 and added to 1.5 * 2^23, a value is rounded to an
+// integer, ties to even, and stands in the low byte of the sum.
+__device__ __forceinline__ uint32_t checkpoint8_quantise4(const float* f, float inv) {
+  uint32_t b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float r = __builtin_amdgcn_fmed3f(f[k] * inv, -127.0f, 127.0f) + 12582912.0f;
+    b[k] = finite_f32(f[k]) ? __builtin_bit_cast(uint32_t, r) : 0x80u;
+  }
+  const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x0C0C0400u);
+  return hi << 16 | lo;
+}
+// The values of N q, a byte each: a byte with its sign bit turned is q + 128, which converts in one instruction.  A zero among those bytes is q = -128, a value that was not finite; words that have one are gone through again.
+template <int N>
+__device__ __forceinline__ void checkpoint8_values(const uint32_t (&v)[N / 4], float scale, float (&f)[N]) {
+  uint32_t zero = 0;
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k) {
+    const uint32_t u = v[k] ^ 0x80808080u;
+    zero |= (u - 0x01010101u) & ~u & 0x80808080u;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) f[4 * k + b] = ((float)((u >> (8 * b)) & 0xFFu) - 128.0f) * scale;
+  }
+  if (zero) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (((v[k >> 2] >> (8 * (k & 3))) & 0xFFu) == 0x80u) f[k] = __builtin_bit_cast(float, 0x7FC00000u);
+  }
 }
 
 typedef uint32_t u32_any_t __attribute__((aligned(1)));
@@ -70,9 +112,7 @@ template <int N>
 __device__ __forceinline__ void store_q(signed char* q, int64_t left, const float (&f)[N], float inv) {
   uint32_t v[N / 4];
 #pragma unroll
-  for (int k = 0; k < N / 4; ++k)
-    v[k] = checkpoint8_quantise(f[4 * k], inv) | checkpoint8_quantise(f[4 * k + 1], inv) << 8 |
-           checkpoint8_quantise(f[4 * k + 2], inv) << 16 | checkpoint8_quantise(f[4 * k + 3], inv) << 24;
+  for (int k = 0; k < N / 4; ++k) v[k] = checkpoint8_quantise4(f + 4 * k, inv);
   if (left >= N) {
 #pragma unroll
     for (int k = 0; k < N / 4; ++k) ((u32_any_t*)q)[k] = v[k];
@@ -95,11 +135,7 @@ __global__ __launch_bounds__(256) void checkpoint8_pack_kernel(const void* x, in
   const int64_t col = b * CKPT8_BLOCK + (c % PER) * N, left = in ? d - col : 0;
   float f[N];
   widen_chunk<DT>(load_chunk<DT>((const char*)x + row * d * Chunk<DT>::BYTES, col, left), f);
-  float m = 0.0f;
-#pragma unroll
-  for (int k = 0; k < N; ++k) m = fmaxf(m, finite_f32(f[k]) ? fabsf(f[k]) : 0.0f);
-#pragma unroll
-  for (int off = 1; off < PER; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  const float m = checkpoint8_top<N, PER>(f);
   if (left <= 0) return;
   const int e = checkpoint8_exponent<DT>(m);
   store_q<N>(q + row * d + col, left, f, power_of_two(-e));
@@ -120,8 +156,7 @@ __global__ __launch_bounds__(256) void checkpoint8_unpack_kernel(const signed ch
   load_q<N>(q + row * d + col, left, v);
   const float scale = power_of_two((int)scales[block] - 127);
   float f[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) f[k] = checkpoint8_value(v[k >> 2], k & 3, scale);
+  checkpoint8_values<N>(v, scale, f);
   store_chunk<DT>((char*)x + row * d * Chunk<DT>::BYTES, col, left, round_chunk<DT>(f));
 }
 

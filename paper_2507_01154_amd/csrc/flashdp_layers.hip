@@ -83,10 +83,11 @@ hipError_t run_vector(VectorArgs& v, char* ws, const VectorWs& w, hipStream_t st
   v.blocks = w.blocks;
   hipError_t e = launch(vector_sum_kernel, v.B * v.blocks, 256, 0, st, v);
   if (e != hipSuccess) return e;
-  const int64_t grid = (v.n + 15) / 16;
-  if (v.B <= VECTOR_FOLD_B && v.B * v.blocks <= VECTOR_FOLD_SQUARES) return launch(vector_clip_kernel<true>, grid, 256, 0, st, v);
-  e = launch(vector_factors_kernel, (v.B + 3) / 4, 256, 0, st, v);
-  return e != hipSuccess ? e : launch(vector_clip_kernel<false>, grid, 256, 0, st, v);
+  const bool fold = v.B <= VECTOR_FOLD_B && v.B * v.blocks <= VECTOR_FOLD_SQUARES;
+  if (!fold && (e = launch(vector_factors_kernel, (v.B + 3) / 4, 256, 0, st, v)) != hipSuccess) return e;
+  // few samples: whole cache lines of elements side by side; many: rows of threads to share them
+  if (v.B <= 16) return launch(fold ? vector_clip_kernel<true, 64> : vector_clip_kernel<false, 64>, (v.n + 63) / 64, 256, 0, st, v);
+  return launch(fold ? vector_clip_kernel<true, 16> : vector_clip_kernel<false, 16>, (v.n + 15) / 16, 256, 0, st, v);
 }
 
 // Tokens per partial sum: about four workgroups per compute unit (column_groups of them per chunk of tokens), and no fewer than
@@ -124,37 +125,66 @@ auto activation_kernel(int act, bool token) {
 
 // ---- layer normalisation ----------------------------------------------------------------------------
 
-// Chunks of 16 bytes a row has decide who holds it: a wave up to 4 chunks a lane, a workgroup up to 8, nobody beyond.
+// Chunks of 16 bytes a row has decide who holds it: a wave up to 4 chunks a lane, a workgroup up to 8, nobody beyond.  Rows that are no whole
+// chunks have fewer kernels to choose from.
 constexpr int64_t NORM_LONG = 256 * 8;
 
 template <int DT>
-void (*norm_kernel(int64_t columns))(const NormArgs) {
-  if (columns <= 64) return layernorm_forward_kernel<DT, 64, 1>;
-  if (columns <= 128) return layernorm_forward_kernel<DT, 64, 2>;
-  if (columns <= 256) return layernorm_forward_kernel<DT, 64, 4>;
-  if (columns <= 512) return layernorm_forward_kernel<DT, 256, 2>;
-  if (columns <= 768) return layernorm_forward_kernel<DT, 256, 3>;
-  if (columns <= 1024) return layernorm_forward_kernel<DT, 256, 4>;
-  return layernorm_forward_kernel<DT, 256, 8>;
-}
-template <int DT>
-void (*norm_grad_kernel(int64_t columns))(const NormGradArgs) {
-  if (columns <= 64) return layernorm_grad_kernel<DT, 64, 1>;
-  if (columns <= 128) return layernorm_grad_kernel<DT, 64, 2>;
-  if (columns <= 256) return layernorm_grad_kernel<DT, 64, 4>;
-  if (columns <= 512) return layernorm_grad_kernel<DT, 256, 2>;
-  if (columns <= 768) return layernorm_grad_kernel<DT, 256, 3>;
-  if (columns <= 1024) return layernorm_grad_kernel<DT, 256, 4>;
-  return layernorm_grad_kernel<DT, 256, 8>;
+void (*norm_kernel(int64_t columns, bool even))(const NormArgs) {
+  if (!even) {
+    if (columns <= 128) return layernorm_forward_kernel<DT, 64, 2, false>;
+    if (columns <= 256) return layernorm_forward_kernel<DT, 64, 4, false>;
+    if (columns <= 1024) return layernorm_forward_kernel<DT, 256, 4, false>;
+    return layernorm_forward_kernel<DT, 256, 8, false>;
+  }
+  if (columns <= 64) return layernorm_forward_kernel<DT, 64, 1, true>;
+  if (columns <= 128) return layernorm_forward_kernel<DT, 64, 2, true>;
+  if (columns <= 256) return layernorm_forward_kernel<DT, 64, 4, true>;
+  if (columns <= 512) return layernorm_forward_kernel<DT, 256, 2, true>;
+  if (columns <= 768) return layernorm_forward_kernel<DT, 256, 3, true>;
+  if (columns <= 1024) return layernorm_forward_kernel<DT, 256, 4, true>;
+  return layernorm_forward_kernel<DT, 256, 8, true>;
 }
 
-struct NormPlan { int64_t columns, col_tiles, chunks, rows_per_chunk; };
+struct NormGradKernel { void (*kernel)(const NormGradArgs); int threads, rows; };   // of a workgroup; rows: that it goes through side by side
+template <int DT, int NT, int CH, int THREADS, bool EVEN>
+NormGradKernel norm_grad_of(bool token) {
+  return {token ? layernorm_grad_kernel<DT, NT, CH, THREADS, true, EVEN> : layernorm_grad_kernel<DT, NT, CH, THREADS, false, EVEN>, THREADS, THREADS / NT};
+}
+template <int DT>
+NormGradKernel norm_grad_kernel(int64_t columns, bool even, bool token) {
+  if (!even) {
+    if (columns <= 128) return norm_grad_of<DT, 64, 2, 256, false>(token);
+    if (columns <= 256) return norm_grad_of<DT, 64, 4, 256, false>(token);
+    if (columns <= 1024) return norm_grad_of<DT, 256, 4, 256, false>(token);
+    return norm_grad_of<DT, 256, 8, 256, false>(token);
+  }
+  if (columns <= 64) return norm_grad_of<DT, 64, 1, 1024, true>(token);
+  if (columns <= 128) return norm_grad_of<DT, 64, 2, 1024, true>(token);
+  if (columns <= 256) return norm_grad_of<DT, 64, 4, 512, true>(token);
+  if (columns <= 512) return norm_grad_of<DT, 256, 2, 1024, true>(token);
+  if (columns <= 768) return norm_grad_of<DT, 256, 3, 1024, true>(token);
+  if (columns <= 1024) return norm_grad_of<DT, 256, 4, 512, true>(token);
+  return norm_grad_of<DT, 256, 8, 256, true>(token);
+}
+NormGradKernel norm_grad_kernel_of(int64_t d, int dtype, bool token) {
+  const int64_t n = chunk_elements(dtype), columns = (d + n - 1) / n;
+  return by_dtype(dtype, [&](auto dt) { return norm_grad_kernel<decltype(dt)::value>(columns, d % n == 0, token); });
+}
+
+struct NormPlan { int64_t columns, col_tiles, chunks, rows_per_chunk; bool token; };
 
 NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   NormPlan p;
   p.columns = (d + chunk_elements(dtype) - 1) / chunk_elements(dtype);
-  p.col_tiles = p.columns > NORM_LONG ? (p.columns + 255) / 256 : 1;
-  const int64_t k = chunks_of(B, T, p.col_tiles);
+  const bool held = p.columns <= NORM_LONG;
+  p.col_tiles = held ? 1 : (p.columns + 255) / 256;
+  p.token = held && T == 1;
+  // about two workgroups of 16 waves per compute unit, each going through its rows at least twice (a partial sum is written and read
+  // for every chunk of rows: 8 x 2048 x 5120 bf16, chunks of 16 rows 135 us, of 32 ...)
+  const NormGradKernel kernel = held ? norm_grad_kernel_of(d, dtype, p.token) : NormGradKernel{nullptr, 256, 8};
+  const int64_t want = (2 * 256 * (1024 / kernel.threads) + B * p.col_tiles - 1) / (B * p.col_tiles);
+  const int64_t k = p.token ? 1 : std::max<int64_t>(1, std::min(want, (T + 2 * kernel.rows - 1) / (2 * kernel.rows)));
   p.rows_per_chunk = (T + k - 1) / k;
   p.chunks = (T + p.rows_per_chunk - 1) / p.rows_per_chunk;
   return p;
@@ -167,15 +197,17 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
 // of at most one workgroup per unit start + alone * k-tiles (fitted to 150 products of one to 8192 rows, 768 to 13824 features; 16-bit types,
 // then fp32, whose k-tiles are half as deep and bound by the matrix cores from 64 x 64 on).  us, in the order of the ladder (- = not tried):
 // bf16 1 x 4096 -> 4096: 7.2, 10.0, 10.0, 14.7, 34, -, -; fp16 8 x 768 -> 50257: 23.3, 16.6, 18.4, 22.4, -, -, -; bf16 128 x 4096 -> 4096: -, -, 14.6, 15.2, 34.9, 46, 74;
-// 256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
+// epilogue: microseconds that an activation or 8-bit sums add to a round (8192 x 768 -> 3072 with GELU and both: -, -, -, 127, 80, 62, 69 beside
+// 109, 62, 51, 51 without).  256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
 // bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; fp32 128 x 4096 -> 4096: -, -, 45, 74, 257, 247, -; 2048 x 4096 -> 4096: -, -, 665, 588, 520, 480, 931.
 // Rows that no 16-byte chunks divide: direct loads to LDS need 4-byte alignment; few rows take the kernel that reads W straight into
 // registers, others tiles staged through registers (bf16 64 x 4096 -> 4096: 23.8, 39.5).
 enum ForwardPath { FWD_16x16 = 0, FWD_16x32, FWD_32x32, FWD_64x64, FWD_128x128, FWD_128x128_TWO, FWD_256x256, FWD_LADDER, FWD_ROWS = FWD_LADDER, FWD_ANY_64, FWD_ANY_128, FWD_PATHS };
-struct ForwardRung { int bm, bn, per_cu; double start, tile, alone, tile32, alone32; };   // tile32 = 0: not for fp32
+struct ForwardRung { int bm, bn, per_cu; double start, tile, alone, tile32, alone32, epilogue; };   // tile32 = 0: not for fp32
 constexpr ForwardRung FORWARD_LADDER[FWD_LADDER] = {
-    {16, 16, 2, 1.9, 0.115, 0.085, 0.115, 0.09}, {16, 32, 3, 2.0, 0.15, 0.12, 0.3, 0.21}, {32, 32, 2, 1.6, 0.18, 0.1, 0.34, 0.2}, {64, 64, 1, 2.6, 0.19, 0.19, 0.56, 0.56},
-    {128, 128, 1, 4.0, 0.54, 0.54, 0.0, 0.0},    {128, 128, 2, 6.6, 0.87, 0.65, 3.7, 1.92},   {256, 256, 1, 7.0, 1.54, 1.54, 0.0, 0.0}};
+    {16, 16, 2, 1.9, 0.115, 0.085, 0.115, 0.09, 0.2}, {16, 32, 3, 2.0, 0.15, 0.12, 0.3, 0.21, 0.3}, {32, 32, 2, 1.6, 0.18, 0.1, 0.34, 0.2, 0.4},
+    {64, 64, 1, 2.6, 0.19, 0.19, 0.56, 0.56, 0.7},    {128, 128, 1, 4.0, 0.54, 0.54, 0.0, 0.0, 2.9}, {128, 128, 2, 6.6, 0.87, 0.65, 3.7, 1.92, 3.7},
+    {256, 256, 1, 7.0, 1.54, 1.54, 0.0, 0.0, 9.0}};
 
 bool forward_direct(int64_t d_in, int dtype) {
   const int64_t kb = d_in * (dtype == FLASHDP_F32 ? 4 : 2);
@@ -187,7 +219,8 @@ int64_t forward_tiles(int64_t rows, int64_t d_out, int bm, int bn) {
   return tm * 8 > GRID_LIMIT || tn * 8 > GRID_LIMIT || tm * tn > GRID_LIMIT ? -1 : tm * tn;
 }
 
-ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, bool blocks_of_32) {
+// blocks_of_32: Z goes out in 8 bits; busy: the epilogue has more to do than to round and store.
+ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, bool blocks_of_32, bool busy) {
   const int forced = api::forward_override();
   if (!forward_direct(d_in, dtype)) {
     if (forced == FWD_ROWS || forced == FWD_ANY_64 || forced == FWD_ANY_128) return forced == FWD_ROWS && rows > 64 ? FWD_ANY_64 : (ForwardPath)forced;
@@ -204,7 +237,8 @@ ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, b
     if (forced == r) return (ForwardPath)r;
     const int64_t slots = cus * g.per_cu, rest = tiles % slots;
     const double tile = dtype == FLASHDP_F32 ? g.tile32 : g.tile, alone = dtype == FLASHDP_F32 ? g.alone32 : g.alone;
-    const double t = (double)(tiles / slots) * (g.start + tile * nk) + (rest == 0 ? 0.0 : g.start + (rest <= cus ? alone : tile) * nk);
+    const double start = g.start + (busy ? g.epilogue : 0.0);
+    const double t = (double)(tiles / slots) * (start + tile * nk) + (rest == 0 ? 0.0 : start + (rest <= cus ? alone : tile) * nk);
     if (best < 0 || t < least) { best = r; least = t; }
   }
   return best < 0 ? FWD_PATHS : (ForwardPath)best;
@@ -267,7 +301,7 @@ int flashdp_linear_forward(const void* X, const void* W, const void* bias, const
   int st = check_rows(rows, d_in);
   if (st == FLASHDP_OK) st = check_rows(rows, d_out);
   if (st != FLASHDP_OK) return st;
-  const ForwardPath path = forward_path(rows, d_in, d_out, dtype, z_8bit != 0);
+  const ForwardPath path = forward_path(rows, d_in, d_out, dtype, z_8bit != 0, activation != FLASHDP_ACT_NONE || z_8bit != 0);
   if (path == FWD_PATHS || (path >= FWD_ANY_64 && forward_tiles(rows, d_out, path == FWD_ANY_64 ? 64 : 128, path == FWD_ANY_64 ? 64 : 128) < 0))
     return FLASHDP_UNSUPPORTED_SHAPE;    // more tiles than a grid holds
   if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(Z, 16)) return FLASHDP_MISALIGNED;
@@ -349,7 +383,7 @@ int flashdp_layernorm_forward(const void* X, const void* gamma, const void* beta
   HIP_TRY(by_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     if (columns > NORM_LONG) return launch(layernorm_forward_long_kernel<DT>, rows, 256, 0, hs, a);
-    return launch(norm_kernel<DT>(columns), columns <= 256 ? (rows + 3) / 4 : rows, 256, 0, hs, a);
+    return launch(norm_kernel<DT>(columns, d % chunk_elements(dtype) == 0), columns <= 256 ? (rows + 3) / 4 : rows, 256, 0, hs, a);
   }));
   api::note_kernel(columns > NORM_LONG ? "layernorm_forward_long_kernel" : "layernorm_forward_kernel");
   return FLASHDP_OK;
@@ -383,10 +417,12 @@ int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, 
   NormGradArgs a;
   a.X = X; a.dY = dY; a.gamma = gamma; a.mean = mean; a.rstd = rstd; a.dX = dX;
   a.partial = out_grad ? reinterpret_cast<float*>(ws + w.partial) : nullptr;
-  a.T = T; a.d = d; a.chunks = (int)p.chunks; a.rows_per_chunk = (int)p.rows_per_chunk; a.bias = bias ? 1 : 0;
-  HIP_TRY(by_dtype(dtype, [&](auto dt) {
+  a.B = B; a.T = T; a.d = d; a.chunks = (int)p.chunks; a.rows_per_chunk = (int)p.rows_per_chunk; a.bias = bias ? 1 : 0;
+  if (p.columns <= NORM_LONG) {
+    const NormGradKernel k = norm_grad_kernel_of(d, dtype, p.token);
+    HIP_TRY(launch(k.kernel, p.token ? (B + k.rows - 1) / k.rows : B * p.chunks, k.threads, 0, hs, a));
+  } else HIP_TRY(by_dtype(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    if (p.columns <= NORM_LONG) return launch(norm_grad_kernel<DT>(p.columns), B * p.chunks, 256, 0, hs, a);
     hipError_t e = hipSuccess;
     if (out_grad) e = launch(layernorm_grad_long_sums_kernel<DT>, B * p.chunks * p.col_tiles, 256, 0, hs, a, (int)p.col_tiles);
     if (e == hipSuccess && dX) e = launch(layernorm_grad_long_rows_kernel<DT>, B * T, 256, 0, hs, a);

@@ -66,32 +66,25 @@ __device__ __forceinline__ void act_chunk(int act, const float (&z)[N], float (&
   }
 }
 
-// The 8-bit form of a chunk of token m, `left` of its features from col on existing (none: the lane only takes part); the lanes
-// of a block of 32 features are neighbours, all of the same token.
+// What becomes of a chunk of sums Z, `left` of which exist (none: the lane only takes part): element `at` of [rows][D] on, block `block` of
+// the 8-bit form.  The lanes of a block of 32 features are neighbours, all of the same token.
 template <int DT>
-__device__ __forceinline__ void keep_chunk8(const ForwardArgs& a, int64_t m, int64_t col, int64_t left, const float (&z)[Chunk<DT>::N]) {
+__device__ __forceinline__ void finish_chunk(const ForwardArgs& a, int64_t at, int64_t block, int left, const float (&z)[Chunk<DT>::N]) {
   constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;
-  float top = 0.0f;
-#pragma unroll
-  for (int k = 0; k < N; ++k) top = fmaxf(top, k < left && finite_f32(z[k]) ? fabsf(z[k]) : 0.0f);
-#pragma unroll
-  for (int off = 1; off < PER; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-  if (left <= 0) return;
-  const int e = checkpoint8_exponent<DT>(top);
-  store_q<N>((signed char*)a.Z + m * a.D + col, left, z, power_of_two(-e));
-  if (col % CKPT8_BLOCK == 0) a.scales[m * checkpoint8_blocks(a.D) + col / CKPT8_BLOCK] = (unsigned char)(e + 127);
-}
-
-// What becomes of a chunk of sums Z of token m, features from col on, `left` of which exist (none: the lane only takes part).
-template <int DT>
-__device__ __forceinline__ void finish_chunk(const ForwardArgs& a, int64_t m, int64_t col, int64_t left, const float (&z)[Chunk<DT>::N]) {
-  constexpr int N = Chunk<DT>::N;
-  const int64_t row = m * a.D * Chunk<DT>::BYTES;
   u32x4_t res = {0u, 0u, 0u, 0u};
-  if (a.residual && left > 0) res = load_chunk<DT>((const char*)a.residual + row, col, left);
-  if (a.keep == KEEP_EIGHT) keep_chunk8<DT>(a, m, col, left, z);
+  if (a.residual && left > 0) res = load_chunk<DT>(a.residual, at, left);
+  if (a.keep == KEEP_EIGHT) {
+    float there[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) there[k] = k < left ? z[k] : 0.0f;
+    const int e = checkpoint8_exponent<DT>(checkpoint8_top<N, PER>(there));
+    if (left > 0) {
+      store_q<N>((signed char*)a.Z + at, left, z, power_of_two(-e));
+      if ((threadIdx.x & (PER - 1)) == 0) a.scales[block] = (unsigned char)(e + 127);
+    }
+  }
   if (left <= 0) return;
-  if (a.keep == KEEP_SAME) store_chunk<DT>((char*)a.Z + row, col, left, round_chunk<DT>(z));
+  if (a.keep == KEEP_SAME) store_chunk<DT>(a.Z, at, left, round_chunk<DT>(z));
   float y[N];
   act_chunk<N>(a.act, z, y);
   if (a.residual) {
@@ -100,7 +93,7 @@ __device__ __forceinline__ void finish_chunk(const ForwardArgs& a, int64_t m, in
 #pragma unroll
     for (int k = 0; k < N; ++k) y[k] += w[k];
   }
-  store_chunk<DT>((char*)a.Y + row, col, left, round_chunk<DT>(y));
+  store_chunk<DT>(a.Y, at, left, round_chunk<DT>(y));
 }
 
 // The end of kernels whose waves share out the k-steps: PARTS partial sums of M tokens x F features in LDS (rows of F + 4 floats) are joined in
@@ -110,7 +103,8 @@ __device__ __forceinline__ void finish_partials(const ForwardArgs& a, const floa
   constexpr int N = Chunk<DT>::N, PITCH = F + 4, PER_ROW = F / N, CHUNKS = M * PER_ROW;
   for (int e = threadIdx.x; e < (CHUNKS + 63) / 64 * 64; e += NT) {
     const int r = CHUNKS % 64 == 0 ? e / PER_ROW : min(e / PER_ROW, M - 1), c = (e % PER_ROW) * N;
-    const int64_t m = m0 + r, col = n0 + c, left = e < CHUNKS && m < a.rows ? a.D - col : 0;
+    const int64_t m = m0 + r;
+    const int col = n0 + c, left = e < CHUNKS && m < a.rows ? a.D - col : 0;
     float z[N];
     widen_chunk<DT>(a.bias ? load_chunk<DT>(a.bias, col, left) : u32x4_t{0u, 0u, 0u, 0u}, z);
 #pragma unroll
@@ -121,7 +115,7 @@ __device__ __forceinline__ void finish_partials(const ForwardArgs& a, const floa
 #pragma unroll
       for (int q = 0; q < 4; ++q) z[k + q] += sum[q];
     }
-    finish_chunk<DT>(a, m, col, left, z);
+    finish_chunk<DT>(a, m * a.D + col, m * checkpoint8_blocks(a.D) + col / CKPT8_BLOCK, left, z);
   }
 }
 
@@ -142,7 +136,9 @@ __device__ __forceinline__ void forward_epilogue(const ForwardArgs& a, const f32
   static_assert(FM % S::BLOCKS == 0 && S::FEATURES % CKPT8_BLOCK == 0, "whole phases, whole blocks of 32 features");
   const int lane = threadIdx.x & 63;
   const int c = (lane % PER_ROW) * N, r0 = lane / PER_ROW;
-  const int64_t col = n0 + c, left = a.D - col;
+  const int col = n0 + c, left = a.D - col;
+  const int64_t blocks = checkpoint8_blocks(a.D);
+  int64_t at = (m0 + r0) * a.D + col, block = (m0 + r0) * blocks + col / CKPT8_BLOCK;
   float b[N];
   widen_chunk<DT>(a.bias ? load_chunk<DT>(a.bias, col, left) : u32x4_t{0u, 0u, 0u, 0u}, b);
 #pragma unroll
@@ -156,8 +152,6 @@ __device__ __forceinline__ void forward_epilogue(const ForwardArgs& a, const f32
 #pragma unroll 2
     for (int it = 0; it < 16 * S::BLOCKS / ROWS; ++it) {
       const int r = it * ROWS + r0;
-      const int64_t m = m0 + 16 * S::BLOCKS * phase + r;
-      const bool ok = m < a.rows && left > 0;
       float z[N];
 #pragma unroll
       for (int k = 0; k < N; k += 4) {
@@ -165,7 +159,9 @@ __device__ __forceinline__ void forward_epilogue(const ForwardArgs& a, const f32
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[k + e] = s[e] + b[k + e];
       }
-      finish_chunk<DT>(a, m, col, ok ? left : 0, z);
+      finish_chunk<DT>(a, at, block, m0 + 16 * S::BLOCKS * phase + r < a.rows ? left : 0, z);
+      at += (int64_t)ROWS * a.D;
+      block += ROWS * blocks;
     }
     __builtin_amdgcn_wave_barrier();
   }

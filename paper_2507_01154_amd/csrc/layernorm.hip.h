@@ -35,16 +35,16 @@ struct NormGradArgs {
   const float* rstd;
   void* dX;               // may be null, may be dY
   float* partial;         // [B][chunks][2 d] (d without a bias); may be null
-  int64_t T, d;
+  int64_t B, T, d;
   int chunks, rows_per_chunk;
   int bias;
 };
 
-// Sums of NV values over the workgroup of 4 waves, the same bits in every thread.  lds: 4 * NV floats that no thread still reads (two
-// buffers in turn need one barrier per sum).
+// Sums of NV values over 256 threads, the same bits in each; several such groups of a workgroup meet at the same barrier.  lds: 4 * NV floats of
+// the group that no thread still reads (two buffers in turn need one barrier per sum).
 template <int NV>
 __device__ __forceinline__ void group_sum(float (&v)[NV], float* lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) & 3;
 #pragma unroll
   for (int k = 0; k < NV; ++k) v[k] = wave_sum(v[k]);
   if (lane == 0)
@@ -55,13 +55,13 @@ __device__ __forceinline__ void group_sum(float (&v)[NV], float* lds) {
   for (int k = 0; k < NV; ++k) v[k] = (lds[k * 4] + lds[k * 4 + 1]) + (lds[k * 4 + 2] + lds[k * 4 + 3]);
 }
 
-// NT threads (64 or 256) share a row, CH chunks each.
-template <int DT, int NT, int CH>
+// NT threads (64 or 256) share a row, CH chunks each.  EVEN: d is whole chunks.
+template <int DT, int NT, int CH, bool EVEN>
 __global__ __launch_bounds__(256) void layernorm_forward_kernel(const NormArgs a) {
   constexpr int N = Chunk<DT>::N;
   __shared__ float lds[2][4];
   const int t = threadIdx.x % NT;
-  const int64_t row = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT;
+  const int64_t row = (int64_t)blockIdx.x * (256 / NT) + __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
   if (row >= a.rows) return;     // NT = 64: a whole wave, and there are no barriers; NT = 256: never
   const char* x = (const char*)a.X + row * a.d * Chunk<DT>::BYTES;
   u32x4_t raw[CH];
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void layernorm_forward_kernel(const NormArgs a
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int64_t col = (int64_t)(c * NT + t) * N;
-    raw[c] = load_chunk<DT>(x, col, a.d - col);
+    raw[c] = load_chunk<DT, EVEN>(x, col, a.d - col);
   }
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void layernorm_forward_kernel(const NormArgs a
     widen_chunk<DT>(raw[c], f);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const float v = k < left ? f[k] - mu : 0.0f;
+      const float v = k < left ? f[k] - mu : 0.0f;     // (EVEN: all or none of a chunk)
       s[0] = fmaf(v, v, s[0]);
     }
   }
@@ -101,11 +101,11 @@ __global__ __launch_bounds__(256) void layernorm_forward_kernel(const NormArgs a
     if (left > 0) {
       float f[N], w[N], b[N];
       widen_chunk<DT>(raw[c], f);
-      widen_chunk<DT>(load_chunk<DT>(a.gamma, col, left), w);
-      widen_chunk<DT>(a.beta ? load_chunk<DT>(a.beta, col, left) : u32x4_t{0u, 0u, 0u, 0u}, b);
+      widen_chunk<DT>(load_chunk<DT, EVEN>(a.gamma, col, left), w);
+      widen_chunk<DT>(a.beta ? load_chunk<DT, EVEN>(a.beta, col, left) : u32x4_t{0u, 0u, 0u, 0u}, b);
 #pragma unroll
       for (int k = 0; k < N; ++k) f[k] = fmaf((f[k] - mu) * r, w[k], b[k]);
-      store_chunk<DT>(y, col, left, round_chunk<DT>(f));
+      store_chunk<DT, EVEN>(y, col, left, round_chunk<DT>(f));
     }
   }
   if (t == 0) {
@@ -156,100 +156,130 @@ __global__ __launch_bounds__(256) void layernorm_forward_long_kernel(const NormA
   }
 }
 
+template <bool EVEN = false>
 __device__ __forceinline__ void store_sums4(float* to, int64_t col, int64_t left, const float* s) {
-  store_chunk<DT_F32>(to, col, left, u32x4_t{__builtin_bit_cast(uint32_t, s[0]), __builtin_bit_cast(uint32_t, s[1]),
+  store_chunk<DT_F32, EVEN>(to, col, left, u32x4_t{__builtin_bit_cast(uint32_t, s[0]), __builtin_bit_cast(uint32_t, s[1]),
                                              __builtin_bit_cast(uint32_t, s[2]), __builtin_bit_cast(uint32_t, s[3])});
 }
 
-// One workgroup per (sample, chunk of tokens): its rows one after the other (NT = 256) or four waves' rows beside each other.
-template <int DT, int NT, int CH>
-__global__ __launch_bounds__(256) void layernorm_grad_kernel(const NormGradArgs a) {
-  constexpr int N = Chunk<DT>::N, ROWS = 256 / NT;
-  __shared__ float lds[NT == 64 ? 4 * 64 * N : 2 * 8];
-  const int t = threadIdx.x % NT;
-  const int64_t i = blockIdx.x / a.chunks, k0 = blockIdx.x - i * a.chunks;
-  const int64_t first = i * a.T + k0 * a.rows_per_chunk;
-  const int64_t last = (k0 + 1) * a.rows_per_chunk < a.T ? first + a.rows_per_chunk : (i + 1) * a.T;
+// NT threads share a row, CH chunks each, THREADS / NT rows side by side.  One workgroup per (sample, chunk of tokens), or with TOKEN
+// (T == 1, a row is a sample) one sample per row of threads, whose sums are the sample's gradient.
+template <int DT, int NT, int CH, int THREADS, bool TOKEN, bool EVEN>
+__global__ __launch_bounds__(THREADS) void layernorm_grad_kernel(const NormGradArgs a) {
+  constexpr int N = Chunk<DT>::N, ROWS = THREADS / NT, PITCH = THREADS + 8;
+  constexpr int JOIN = TOKEN || ROWS == 1 ? 0 : N * PITCH, SUMS = NT == 64 ? 0 : 2 * ROWS * 8;
+  __shared__ float lds[JOIN > SUMS ? JOIN : SUMS > 0 ? SUMS : 1];
+  const int t = threadIdx.x % NT, g = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);   // (whole waves share a row)
+  int64_t first, last;
+  if constexpr (TOKEN) {
+    first = (int64_t)blockIdx.x * ROWS;
+    last = first + ROWS < a.B ? first + ROWS : a.B;
+  } else {
+    const int64_t i = blockIdx.x / a.chunks, k0 = blockIdx.x - i * a.chunks;
+    first = i * a.T + k0 * a.rows_per_chunk;
+    last = (k0 + 1) * a.rows_per_chunk < a.T ? first + a.rows_per_chunk : (i + 1) * a.T;
+  }
   const float per_d = 1.0f / (float)a.d;
+  const int64_t pitch = a.d * Chunk<DT>::BYTES;
   u32x4_t w[CH];
   float sg[CH][N], sb[CH][N];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int64_t col = (int64_t)(c * NT + t) * N;
-    w[c] = load_chunk<DT>(a.gamma, col, a.d - col);
+    w[c] = load_chunk<DT, EVEN>(a.gamma, col, a.d - col);
 #pragma unroll
     for (int k = 0; k < N; ++k) sg[c][k] = sb[c][k] = 0.0f;
   }
   int turn = 0;
-  for (int64_t row = first + threadIdx.x / NT; row < last; row += ROWS) {
-    const char* x = (const char*)a.X + row * a.d * Chunk<DT>::BYTES;
-    const char* dy = (const char*)a.dY + row * a.d * Chunk<DT>::BYTES;
+  for (int64_t row0 = first; row0 < last; row0 += ROWS) {     // the same number of times for all rows of threads: they meet at barriers
+    const int64_t row = row0 + g;      // (scalar, so that addresses cost no vector registers)
+    const bool in = row < last;
+    const char* x = (const char*)a.X + row * pitch;
+    const char* dy = (const char*)a.dY + row * pitch;
     u32x4_t xr[CH], gr[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int64_t col = (int64_t)(c * NT + t) * N;
-      xr[c] = load_chunk<DT>(x, col, a.d - col);
-      gr[c] = load_chunk<DT>(dy, col, a.d - col);
+      const int64_t col = (int64_t)(c * NT + t) * N, left = in ? a.d - col : 0;
+      xr[c] = load_chunk<DT, EVEN>(x, col, left);
+      gr[c] = load_chunk<DT, EVEN>(dy, col, left);
     }
-    const float mu = a.mean[row], r = a.rstd[row];
+    const float mu = in ? a.mean[row] : 0.0f, r = in ? a.rstd[row] : 0.0f;
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float f[N], g[N], v[N];
+      float f[N], e[N], v[N];
       widen_chunk<DT>(xr[c], f);
-      widen_chunk<DT>(gr[c], g);
+      widen_chunk<DT>(gr[c], e);
       widen_chunk<DT>(w[c], v);
 #pragma unroll
-      for (int k = 0; k < N; ++k) {     // (columns that do not exist have dy = gamma = 0)
-        const float xh = (f[k] - mu) * r, p = g[k] * v[k];
+      for (int k = 0; k < N; ++k) {     // (columns and rows that do not exist have dy = 0)
+        const float xh = (f[k] - mu) * r, p = e[k] * v[k];
         s[0] += p;
         s[1] = fmaf(p, xh, s[1]);
-        sg[c][k] = fmaf(g[k], xh, sg[c][k]);
-        sb[c][k] += g[k];
+        sg[c][k] = fmaf(e[k], xh, sg[c][k]);
+        sb[c][k] += e[k];
       }
+      // (added up here: left to the compiler, the sums over tokens wait behind the barrier, with the widened row in registers)
+#pragma unroll
+      for (int k = 0; k < N; ++k) asm volatile("" : "+v"(sg[c][k]), "+v"(sb[c][k]));
     }
     if constexpr (NT == 64) { s[0] = wave_sum(s[0]); s[1] = wave_sum(s[1]); }
-    else { group_sum(s, lds + 8 * turn); turn ^= 1; }
-    if (a.dX) {
+    else { group_sum(s, lds + (turn * ROWS + g) * 8); turn ^= 1; }
+    // (kept as they were loaded, and widened again: the widened row beside the sums would not fit the registers)
+#pragma unroll
+    for (int c = 0; c < CH; ++c) asm volatile("" : "+v"(xr[c]), "+v"(gr[c]), "+v"(w[c]));
+    if (a.dX && in) {
       const float m0 = s[0] * per_d, m1 = s[1] * per_d;
-      char* dx = (char*)a.dX + row * a.d * Chunk<DT>::BYTES;
+      char* dx = (char*)a.dX + row * pitch;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
         if (left > 0) {
-          float f[N], g[N], v[N];
+          float f[N], e[N], v[N];
           widen_chunk<DT>(xr[c], f);
-          widen_chunk<DT>(gr[c], g);
+          widen_chunk<DT>(gr[c], e);
           widen_chunk<DT>(w[c], v);
 #pragma unroll
-          for (int k = 0; k < N; ++k) f[k] = r * (fmaf(g[k], v[k], -m0) - (f[k] - mu) * r * m1);
-          store_chunk<DT>(dx, col, left, round_chunk<DT>(f));
+          for (int k = 0; k < N; ++k) f[k] = r * (fmaf(e[k], v[k], -m0) - (f[k] - mu) * r * m1);
+          store_chunk<DT, EVEN>(dx, col, left, round_chunk<DT>(f));
         }
       }
     }
   }
   if (!a.partial) return;
-  float* to = a.partial + (int64_t)blockIdx.x * a.d * (a.bias ? 2 : 1);
+  if constexpr (TOKEN || ROWS == 1) {
+    if (TOKEN && first + g >= last) return;
+    float* to = a.partial + (TOKEN ? first + g : (int64_t)blockIdx.x) * a.d * (a.bias ? 2 : 1);
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
+    for (int c = 0; c < CH; ++c) {
+      const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      if (part == 1 && !a.bias) break;
-      float* s = part ? sb[c] : sg[c];
-      if constexpr (NT == 64) {     // the four waves' sums, joined by the first
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < N; ++k) lds[k * 256 + threadIdx.x] = s[k];
-        __syncthreads();
-        if (threadIdx.x >= 64) continue;
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-          s[k] = (lds[k * 256 + t] + lds[k * 256 + 64 + t]) + (lds[k * 256 + 128 + t] + lds[k * 256 + 192 + t]);
+      for (int q = 0; q < N; q += 4) {
+        store_sums4<EVEN>(to, col + q, left - q, sg[c] + q);
+        if (a.bias) store_sums4<EVEN>(to + a.d, col + q, left - q, sb[c] + q);
       }
-      if (left > 0)
+    }
+  } else {
+    // the rows of threads join their sums, NT * N columns of one of the two vectors at a time
+    float* to = a.partial + (int64_t)blockIdx.x * a.d * (a.bias ? 2 : 1);
 #pragma unroll
-        for (int q = 0; q < N / 4; ++q) store_sums4(to + part * a.d, col + 4 * q, left - 4 * q, s + 4 * q);
+    for (int c = 0; c < CH; ++c) {
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        if (part == 1 && !a.bias) break;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) lds[k * PITCH + threadIdx.x] = part ? sb[c][k] : sg[c][k];
+        __syncthreads();
+        for (int e = threadIdx.x; e < NT * N; e += THREADS) {
+          const int64_t col = (int64_t)c * NT * N + e;
+          if (col >= a.d) break;
+          float s = 0.0f;
+#pragma unroll
+          for (int q = 0; q < ROWS; ++q) s += lds[(e % N) * PITCH + q * NT + e / N];
+          to[part * a.d + col] = s;
+        }
+      }
     }
   }
 }

@@ -51,11 +51,14 @@ __global__ __launch_bounds__(256) void vector_sum_kernel(const VectorArgs a) {
   if (lane == 0) a.squares[blockIdx.x] = q;
 }
 
-__device__ __forceinline__ double vector_norm(const double* __restrict__ squares_i, int blocks, int lane) {
+// The norm of sample i by `lanes` (a power of two) neighbouring lanes, of which this one is number `lane`; the same in all of them.
+__device__ __forceinline__ double vector_norm(const VectorArgs& a, int64_t i, int lane, int lanes) {
+  const double* q = a.squares + i * a.blocks;
   double s = 0.0;
 #pragma unroll 4
-  for (int k = lane; k < blocks; k += 64) s += squares_i[k];
-  return sqrt(wave_sum(s));
+  for (int k = lane; k < a.blocks; k += lanes) s += q[k];
+  for (int off = lanes >> 1; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+  return sqrt(s);
 }
 
 // Clip factors in a launch of their own, one wave per sample.
@@ -63,45 +66,50 @@ __global__ __launch_bounds__(256) void vector_factors_kernel(const VectorArgs a)
   const int lane = threadIdx.x & 63;
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= a.B) return;
-  const double n = vector_norm(a.squares + i * a.blocks, a.blocks, lane);
+  const double n = vector_norm(a, i, lane, 64);
   if (lane == 0) {
     a.factors[i] = clip_factor_of(n, a.C);
     if (a.out_norms) a.out_norms[i] = (float)n;
   }
 }
 
-// out for 16 elements per workgroup: 16 threads of it side by side, the samples dealt to 16 rows of threads and their sums
-// joined in a fixed order.  FOLD: every workgroup works the clip factors out for itself.
+// out for COLS elements per workgroup: COLS threads of it side by side, the samples dealt to 256 / COLS rows of threads and their sums
+// joined in a fixed order.  FOLD: every workgroup works the clip factors out for itself, all samples at a time (256 / B lanes each;
+// a wave for one sample after the other takes a microsecond each: 256 samples of 512 elements 40 us, 3 so).
 constexpr int VECTOR_FOLD_B = 1024;             // factors kept in LDS
 constexpr int64_t VECTOR_FOLD_SQUARES = 8192;   // B * blocks doubles that every workgroup reads: 64 KB from the caches
-template <bool FOLD>
+template <bool FOLD, int COLS>
 __global__ __launch_bounds__(256) void vector_clip_kernel(const VectorArgs a) {
+  constexpr int ROWS = 256 / COLS;
   __shared__ float fac[FOLD ? VECTOR_FOLD_B : 1];
-  __shared__ float part[16][16];
+  __shared__ float part[ROWS][COLS];
   if constexpr (FOLD) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t i = threadIdx.x >> 6; i < a.B; i += 4) {
-      const double n = vector_norm(a.squares + i * a.blocks, a.blocks, lane);
-      if (lane == 0) {
+    int lanes = 64;
+    while (lanes > 1 && lanes * a.B > 256) lanes >>= 1;
+    const int lane = threadIdx.x & (lanes - 1);
+    for (int64_t i0 = 0; i0 < a.B; i0 += 256 / lanes) {      // (whole waves take part in the sums of lanes)
+      const int64_t i = i0 + threadIdx.x / lanes;
+      const double n = vector_norm(a, i < a.B ? i : a.B - 1, lane, lanes);
+      if (lane == 0 && i < a.B) {
         fac[i] = clip_factor_of(n, a.C);
         if (blockIdx.x == 0 && a.out_norms) a.out_norms[i] = (float)n;
       }
     }
     __syncthreads();
   }
-  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
-  const int64_t col = (int64_t)blockIdx.x * 16 + c;
+  const int c = threadIdx.x % COLS, r = threadIdx.x / COLS;
+  const int64_t col = (int64_t)blockIdx.x * COLS + c;
   float s = 0.0f;
   if (col < a.n) {
-#pragma unroll 4
-    for (int64_t i = r; i < a.B; i += 16) s = fmaf(FOLD ? fac[i] : a.factors[i], a.g[i * a.n + col], s);
+#pragma unroll 8
+    for (int64_t i = r; i < a.B; i += ROWS) s = fmaf(FOLD ? fac[i] : a.factors[i], a.g[i * a.n + col], s);
   }
   part[r][c] = s;
   __syncthreads();
   if (r != 0 || col >= a.n) return;
   s = 0.0f;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) s += part[k][c];
+  for (int k = 0; k < ROWS; ++k) s += part[k][c];
   if (a.accumulate) s += a.out[col];
   if (a.noise_scale != 0.0f) {
     const Normals4 z = noise_group(a.seed, a.layer, (uint64_t)(col >> 2), a.field);
