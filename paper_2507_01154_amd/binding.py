@@ -318,12 +318,15 @@ def flashdp_mfma_probe(pattern: int, iters: int, workgroups: int, sink, stream=N
 # ---- the layers around the weight gradient ----------------------------------------------------------
 
 _FLOATS = {}
+_torch = None
 
 
 def _float_type(dtype: int):
-    import torch
-    if not _FLOATS:
+    global _torch
+    if _torch is None:
+        import torch
         _FLOATS.update({BF16: torch.bfloat16, F32: torch.float32, F16: torch.float16})
+        _torch = torch
     return _FLOATS.get(dtype)
 
 
@@ -338,11 +341,14 @@ def _buffer(t, n: int, dtype, where: str) -> Optional[int]:
     return t.data_ptr()
 
 
-def _current(t, where: str):
-    """The library works on the current device; so has the caller's tensor to be."""
-    import torch
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _here(t, stream, where: str) -> Optional[int]:
+    """Handle of the stream to enqueue on.  The library works on the current device; so has the caller's tensor to be."""
+    device = t.get_device()
+    if device < 0 or device != _torch.cuda.current_device():
         raise FlashDPError(INVALID_ARGUMENT, f"{where}: the tensors are on {t.device}, which is not the current device")
+    if stream is None:
+        return _torch._C._cuda_getCurrentRawStream(device) or None      # (torch.cuda.current_stream() makes an object, a microsecond)
+    return _stream_handle(stream)
 
 
 def _room(workspace):
@@ -353,13 +359,12 @@ def flashdp_linear_forward(X, W, bias, residual, rows: int, d_in: int, d_out: in
                            stream=None):
     """Y = act(X W^T + bias) + residual; Z, if given, receives X W^T + bias, in the call's type or as an 8-bit checkpoint (a uint8
     tensor of flashdp_checkpoint8_bytes(rows, d_out)).  activation: a name or code."""
-    import torch
     w, f = "flashdp_linear_forward", _float_type(dtype)
-    _current(X, w)
-    z = _buffer(Z, flashdp_checkpoint8_bytes(rows, d_out), torch.uint8, w) if z_8bit else _buffer(Z, rows * d_out, f, w)
+    st = _here(X, stream, w)
+    z = _buffer(Z, flashdp_checkpoint8_bytes(rows, d_out), _torch.uint8, w) if z_8bit else _buffer(Z, rows * d_out, f, w)
     _check(lib().flashdp_linear_forward(_buffer(X, rows * d_in, f, w), _buffer(W, d_out * d_in, f, w), _buffer(bias, d_out, f, w),
                                         _buffer(residual, rows * d_out, f, w), rows, d_in, d_out, int(dtype), activation_code(activation),
-                                        _buffer(Y, rows * d_out, f, w), z, int(bool(z_8bit)), _stream_handle(stream)), w)
+                                        _buffer(Y, rows * d_out, f, w), z, int(bool(z_8bit)), st), w)
 
 
 def flashdp_activation_workspace_bytes(B: int, T: int, d_out: int, dtype: int) -> int:
@@ -369,24 +374,21 @@ def flashdp_activation_workspace_bytes(B: int, T: int, d_out: int, dtype: int) -
 def flashdp_activation_dp_grad(dY, Z, z_8bit: bool, B: int, T: int, d_out: int, dtype: int, activation, C: float, sigma: float, seed: int, layer: int,
                                dZ, out_grad, out_norms=None, workspace=None, stream=None, accumulate: bool = False, add_noise: bool = True):
     """dZ = dY act'(Z) and the clipped, noised gradient of the bias (out_grad [d_out] fp32, or None)."""
-    import torch
     w, f, n = "flashdp_activation_dp_grad", _float_type(dtype), B * T * d_out
-    _current(dY, w)
-    z = _buffer(Z, flashdp_checkpoint8_bytes(B * T, d_out), torch.uint8, w) if z_8bit else _buffer(Z, n, f, w)
+    st = _here(dY, stream, w)
+    z = _buffer(Z, flashdp_checkpoint8_bytes(B * T, d_out), _torch.uint8, w) if z_8bit else _buffer(Z, n, f, w)
     ws, ws_bytes = _room(workspace)
     _check(lib().flashdp_activation_dp_grad(_buffer(dY, n, f, w), z, int(bool(z_8bit)), B, T, d_out, int(dtype), activation_code(activation), C, sigma, seed, layer,
-                                            _buffer(dZ, n, f, w), _buffer(out_grad, d_out, torch.float32, w), _buffer(out_norms, B, torch.float32, w),
-                                            ws, ws_bytes, _stream_handle(stream), int(bool(accumulate)), int(bool(add_noise))), w)
+                                            _buffer(dZ, n, f, w), _buffer(out_grad, d_out, _torch.float32, w), _buffer(out_norms, B, _torch.float32, w),
+                                            ws, ws_bytes, st, int(bool(accumulate)), int(bool(add_noise))), w)
 
 
 def flashdp_layernorm_forward(X, gamma, beta, rows: int, d: int, dtype: int, eps: float, Y, mean=None, rstd=None, stream=None):
     """Y = (X - mean) rstd gamma + beta over rows of d features; mean and rstd [rows] fp32 are kept for the backward pass if given."""
-    import torch
     w, f = "flashdp_layernorm_forward", _float_type(dtype)
-    _current(X, w)
+    st = _here(X, stream, w)
     _check(lib().flashdp_layernorm_forward(_buffer(X, rows * d, f, w), _buffer(gamma, d, f, w), _buffer(beta, d, f, w), rows, d, int(dtype), eps,
-                                           _buffer(Y, rows * d, f, w), _buffer(mean, rows, torch.float32, w), _buffer(rstd, rows, torch.float32, w),
-                                           _stream_handle(stream)), w)
+                                           _buffer(Y, rows * d, f, w), _buffer(mean, rows, _torch.float32, w), _buffer(rstd, rows, _torch.float32, w), st), w)
 
 
 def flashdp_layernorm_workspace_bytes(B: int, T: int, d: int, dtype: int, bias: bool = True) -> int:
@@ -396,14 +398,13 @@ def flashdp_layernorm_workspace_bytes(B: int, T: int, d: int, dtype: int, bias: 
 def flashdp_layernorm_dp_grad(X, dY, gamma, mean, rstd, B: int, T: int, d: int, dtype: int, C: float, sigma: float, seed: int, layer: int, dX, out_grad,
                               out_norms=None, bias: bool = True, workspace=None, stream=None, accumulate: bool = False, add_noise: bool = True):
     """dX and the clipped, noised gradient of gamma and beta (out_grad [2, d] fp32; [d] without a bias; or None)."""
-    import torch
     w, f, n = "flashdp_layernorm_dp_grad", _float_type(dtype), B * T * d
-    _current(X, w)
+    st = _here(X, stream, w)
     ws, ws_bytes = _room(workspace)
-    _check(lib().flashdp_layernorm_dp_grad(_buffer(X, n, f, w), _buffer(dY, n, f, w), _buffer(gamma, d, f, w), _buffer(mean, B * T, torch.float32, w),
-                                           _buffer(rstd, B * T, torch.float32, w), B, T, d, int(dtype), C, sigma, seed, layer, _buffer(dX, n, f, w),
-                                           _buffer(out_grad, (2 if bias else 1) * d, torch.float32, w), _buffer(out_norms, B, torch.float32, w), int(bool(bias)),
-                                           ws, ws_bytes, _stream_handle(stream), int(bool(accumulate)), int(bool(add_noise))), w)
+    _check(lib().flashdp_layernorm_dp_grad(_buffer(X, n, f, w), _buffer(dY, n, f, w), _buffer(gamma, d, f, w), _buffer(mean, B * T, _torch.float32, w),
+                                           _buffer(rstd, B * T, _torch.float32, w), B, T, d, int(dtype), C, sigma, seed, layer, _buffer(dX, n, f, w),
+                                           _buffer(out_grad, (2 if bias else 1) * d, _torch.float32, w), _buffer(out_norms, B, _torch.float32, w), int(bool(bias)),
+                                           ws, ws_bytes, st, int(bool(accumulate)), int(bool(add_noise))), w)
 
 
 def flashdp_checkpoint8_bytes(rows: int, d: int) -> int:
@@ -411,19 +412,17 @@ def flashdp_checkpoint8_bytes(rows: int, d: int) -> int:
 
 
 def flashdp_checkpoint8_pack(X, rows: int, d: int, dtype: int, packed, stream=None):
-    import torch
-    w = "flashdp_checkpoint8_pack"
-    _current(X, w)
-    _check(lib().flashdp_checkpoint8_pack(_buffer(X, rows * d, _float_type(dtype), w), rows, d, int(dtype),
-                                          _buffer(packed, flashdp_checkpoint8_bytes(rows, d), torch.uint8, w), _stream_handle(stream)), w)
+    w, f = "flashdp_checkpoint8_pack", _float_type(dtype)
+    st = _here(X, stream, w)
+    _check(lib().flashdp_checkpoint8_pack(_buffer(X, rows * d, f, w), rows, d, int(dtype),
+                                          _buffer(packed, flashdp_checkpoint8_bytes(rows, d), _torch.uint8, w), st), w)
 
 
 def flashdp_checkpoint8_unpack(packed, rows: int, d: int, dtype: int, X, stream=None):
-    import torch
-    w = "flashdp_checkpoint8_unpack"
-    _current(packed, w)
-    _check(lib().flashdp_checkpoint8_unpack(_buffer(packed, flashdp_checkpoint8_bytes(rows, d), torch.uint8, w), rows, d, int(dtype),
-                                            _buffer(X, rows * d, _float_type(dtype), w), _stream_handle(stream)), w)
+    w, f = "flashdp_checkpoint8_unpack", _float_type(dtype)
+    st = _here(packed, stream, w)
+    _check(lib().flashdp_checkpoint8_unpack(_buffer(packed, flashdp_checkpoint8_bytes(rows, d), _torch.uint8, w), rows, d, int(dtype),
+                                            _buffer(X, rows * d, f, w), st), w)
 
 
 def flashdp_workspace_bytes_checkpoint8(layers, B: int, T: int, dtype: int, schedule=SCHEDULE_SCRATCH) -> int:
@@ -434,17 +433,18 @@ def flashdp_workspace_bytes_checkpoint8(layers, B: int, T: int, dtype: int, sche
 def flashdp_block_dp_grad_checkpoint8(layers, B: int, T: int, dtype: int, schedule=SCHEDULE_AUTO, workspace=None, stream=None,
                                       accumulate: bool = False, add_noise: bool = True):
     """flashdp_block_dp_grad_micro with each layer's X an 8-bit checkpoint (a uint8 tensor of flashdp_checkpoint8_bytes(B * T, d_in))."""
-    import torch
-    w = "flashdp_block_dp_grad_checkpoint8"
-    arr = layers
+    w, f = "flashdp_block_dp_grad_checkpoint8", _float_type(dtype)
+    arr, st = layers, None
     if isinstance(layers, (list, tuple)):
         for L in layers:
-            _current(L["X"], w)
-            _buffer(L["X"], flashdp_checkpoint8_bytes(B * T, L["d_in"]), torch.uint8, w)
-            _buffer(L["dY"], B * T * L["d_out"], _float_type(dtype), w)
-            _buffer(L["out_grad"], L["d_in"] * L["d_out"], torch.float32, w)
-            _buffer(L.get("out_norms"), B, torch.float32, w)
+            st = _here(L["X"], stream, w)
+            _buffer(L["X"], flashdp_checkpoint8_bytes(B * T, L["d_in"]), _torch.uint8, w)
+            _buffer(L["dY"], B * T * L["d_out"], f, w)
+            _buffer(L["out_grad"], L["d_in"] * L["d_out"], _torch.float32, w)
+            _buffer(L.get("out_norms"), B, _torch.float32, w)
         arr = make_layers(layers)
+    else:
+        st = _stream_handle(stream)
     ws, ws_bytes = _room(workspace)
-    _check(lib().flashdp_block_dp_grad_checkpoint8(arr, len(arr), B, T, int(dtype), schedule_code(schedule), ws, ws_bytes, _stream_handle(stream),
+    _check(lib().flashdp_block_dp_grad_checkpoint8(arr, len(arr), B, T, int(dtype), schedule_code(schedule), ws, ws_bytes, st,
                                                    int(bool(accumulate)), int(bool(add_noise))), w)

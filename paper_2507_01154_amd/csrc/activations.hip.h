@@ -6,8 +6,8 @@
 //   SiLU              z s(z)
 //   GELU              z erfc(-z / sqrt(2)) / 2
 // s(v) = 1 / (1 + e^-v): for v << 0 the exponential overflows to infinity and s is 0.  All of them have reached their limits
-// in fp32 at |z| = 128, where arguments are cut off, so that infinities give the limit and not 0 times infinity; NaN
-// stays NaN (every comparison with it is false).
+// in fp32 at |z| = 128, where the factors beside the step are cut off, so that infinities give the limit and not 0 times infinity; the step
+// itself is taken of z as it is, so NaN stays NaN though minima and maxima drop it.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -20,26 +20,26 @@ __device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcp
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
   if constexpr (ACT == ACT_NONE) return z;
-  if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : z;
-  z = z < -128.0f ? -128.0f : z;
-  if constexpr (ACT == ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
-  if constexpr (ACT == ACT_GELU_TANH) return z * logistic(1.5957691f * z * fmaf(0.044715f * z, z, 1.0f));
-  if constexpr (ACT == ACT_SILU) return z * logistic(z);
+  if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : z;     // (a comparison with NaN is false)
+  const float c = fmaxf(z, -128.0f);
+  if constexpr (ACT == ACT_GELU) return 0.5f * c * erfcf(-0.70710678f * z);
+  if constexpr (ACT == ACT_GELU_TANH) return c * logistic(1.5957691f * z * fmaf(0.044715f * z, z, 1.0f));
+  if constexpr (ACT == ACT_SILU) return c * logistic(z);
 }
 
 template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
   if constexpr (ACT == ACT_NONE) return 1.0f;
   if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : z > 0.0f ? 1.0f : z;
-  z = z < -128.0f ? -128.0f : z > 128.0f ? 128.0f : z;
-  if constexpr (ACT == ACT_GELU) return fmaf(0.39894228f * z, __expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678f * z));
+  const float c = __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f);
+  if constexpr (ACT == ACT_GELU) return fmaf(0.39894228f * c, __expf(-0.5f * c * c), 0.5f * erfcf(-0.70710678f * z));
   if constexpr (ACT == ACT_GELU_TANH) {
-    const float zz = z * z, s = logistic(1.5957691f * z * fmaf(0.044715f, zz, 1.0f));
-    return fmaf(z * 1.5957691f * fmaf(3.0f * 0.044715f, zz, 1.0f) * (1.0f - s), s, s);   // s + z s (1 - s) d(2 u)/dz
+    const float cc = c * c, s = logistic(1.5957691f * z * fmaf(0.044715f * c, c, 1.0f));
+    return fmaf(c * 1.5957691f * fmaf(3.0f * 0.044715f, cc, 1.0f) * (1.0f - s), s, s);   // s + z s (1 - s) d(2 u)/dz
   }
   if constexpr (ACT == ACT_SILU) {
     const float s = logistic(z);
-    return fmaf(z * (1.0f - s), s, s);
+    return fmaf(c * (1.0f - s), s, s);
   }
 }
 

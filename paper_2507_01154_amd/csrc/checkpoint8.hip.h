@@ -44,10 +44,11 @@ __device__ __forceinline__ uint32_t max_of_lanes(uint32_t m) {
   return PER == 8 ? max(m, lane_exchange<LANE_REVERSE_8>(m)) : m;
 }
 
-// The largest finite magnitude of N values, agreed on by PER neighbouring lanes that hold a block; values from `left` on do not exist (zeros).
-// Magnitudes are compared as integers; only a block that has a value which is not finite is gone through again without it.
+// Bits of the largest magnitude of N values of a block that PER neighbouring lanes hold, agreed on by them (magnitudes compare as integers).
+// From CKPT8_NOT_FINITE on, the block has a value that is not finite: the top bit is set then, below it the bits of the largest finite one.
+constexpr uint32_t CKPT8_NOT_FINITE = 0x80000000u;
 template <int N, int PER>
-__device__ __forceinline__ float checkpoint8_top(const float (&f)[N]) {
+__device__ __forceinline__ uint32_t checkpoint8_top(const float (&f)[N]) {
   uint32_t m = 0;
 #pragma unroll
   for (int k = 0; k < N; ++k) m = max(m, __builtin_bit_cast(uint32_t, f[k]) & 0x7FFFFFFFu);
@@ -56,22 +57,20 @@ __device__ __forceinline__ float checkpoint8_top(const float (&f)[N]) {
     m = 0;
 #pragma unroll
     for (int k = 0; k < N; ++k) m = max(m, finite_f32(f[k]) ? __builtin_bit_cast(uint32_t, f[k]) & 0x7FFFFFFFu : 0u);
-    m = max_of_lanes<PER>(m);
+    m = max_of_lanes<PER>(m) | CKPT8_NOT_FINITE;
   }
-  return __builtin_bit_cast(float, m);
+  return m;
 }
-// Four q, a byte each, of values in a block of scale 2^-e = inv.  Cut to -127 .. 127 and added to 1.5 * 2^23, a value is rounded to an
+// Four q, a byte each, of finite values in a block of scale 2^-e = inv.  Cut to -127 .. 127 and added to 1.5 * 2^23, a value is rounded to an
 // integer, ties to even, and stands in the low byte of the sum.
 __device__ __forceinline__ uint32_t checkpoint8_quantise4(const float* f, float inv) {
   uint32_t b[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float r = __builtin_amdgcn_fmed3f(f[k] * inv, -127.0f, 127.0f) + 12582912.0f;
-    b[k] = finite_f32(f[k]) ? __builtin_bit_cast(uint32_t, r) : 0x80u;
-  }
+  for (int k = 0; k < 4; ++k) b[k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(f[k] * inv, -127.0f, 127.0f) + 12582912.0f);
   const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x0C0C0400u);
   return hi << 16 | lo;
 }
+
 // The values of N q, a byte each: a byte with its sign bit turned is q + 128, which converts in one instruction.  A zero among those bytes is q = -128, a value that was not finite; words that have one are gone through again.
 template <int N>
 __device__ __forceinline__ void checkpoint8_values(const uint32_t (&v)[N / 4], float scale, float (&f)[N]) {
@@ -107,12 +106,20 @@ __device__ __forceinline__ void load_q(const signed char* q, int64_t left, uint3
   }
 }
 
-// The q of N values of scale 2^e = 1 / inv to q[0 ..], `left` of which exist.
-template <int N>
-__device__ __forceinline__ void store_q(signed char* q, int64_t left, const float (&f)[N], float inv) {
+// The q of a chunk of a block with the given top (checkpoint8_top) to q[0 ..], `left` > 0 of which exist; returns the block's e.
+template <int DT>
+__device__ __forceinline__ int checkpoint8_keep(signed char* q, int left, const float (&f)[Chunk<DT>::N], uint32_t top) {
+  constexpr int N = Chunk<DT>::N;
+  const int e = checkpoint8_exponent<DT>(__builtin_bit_cast(float, top & ~CKPT8_NOT_FINITE));
+  const float inv = power_of_two(-e);
   uint32_t v[N / 4];
 #pragma unroll
   for (int k = 0; k < N / 4; ++k) v[k] = checkpoint8_quantise4(f + 4 * k, inv);
+  if (top >= CKPT8_NOT_FINITE) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (!finite_f32(f[k])) v[k >> 2] = (v[k >> 2] & ~(0xFFu << (8 * (k & 3)))) | 0x80u << (8 * (k & 3));
+  }
   if (left >= N) {
 #pragma unroll
     for (int k = 0; k < N / 4; ++k) ((u32_any_t*)q)[k] = v[k];
@@ -121,43 +128,47 @@ __device__ __forceinline__ void store_q(signed char* q, int64_t left, const floa
     for (int k = 0; k < N - 1; ++k)
       if (k < left) q[k] = (signed char)(v[k >> 2] >> (8 * (k & 3)));
   }
+  return e;
 }
 
-// One thread per chunk of 16 bytes of x; the chunks of a row fill whole blocks (chunks past the row's end hold zeros and store
-// nothing), so the lanes of a block are neighbours in one wave.
-template <int DT>
-__global__ __launch_bounds__(256) void checkpoint8_pack_kernel(const void* x, int64_t rows, int64_t d, signed char* q, unsigned char* scales) {
-  constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;   // chunks per block
-  const int64_t nb = checkpoint8_blocks(d), chunks = rows * nb * PER;
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const bool in = c < chunks;
-  const int64_t block = in ? c / PER : 0, row = block / nb, b = block - row * nb;
-  const int64_t col = b * CKPT8_BLOCK + (c % PER) * N, left = in ? d - col : 0;
+// One chunk of 16 bytes of x per thread (two or four, a workgroup apart: 16384 x 5120 bf16 packed and unpacked 97.7 us, 90.1 so).  The chunks of
+// a row fill whole blocks (chunks past the row's end hold zeros and store nothing), so the lanes of a block are neighbours in one wave.
+// FLAT: d is whole blocks, and chunk c is simply elements N c on; otherwise a chunk's place costs a division (93.5 us).
+struct Checkpoint8Place { int64_t at, block; int left; };   // element, block, elements that exist
+template <int N, bool FLAT>
+__device__ __forceinline__ Checkpoint8Place checkpoint8_place(int64_t c, int64_t chunks, int64_t d) {
+  constexpr int PER = CKPT8_BLOCK / N;   // chunks per block
+  const int64_t block = c / PER;
+  if (c >= chunks) return {0, 0, 0};
+  if constexpr (FLAT) return {c * N, block, N};
+  const int64_t nb = checkpoint8_blocks(d), row = block / nb;
+  const int64_t col = (block - row * nb) * CKPT8_BLOCK + (c % PER) * N;
+  return {row * d + col, block, (int)max((int64_t)0, min((int64_t)N, d - col))};
+}
+
+template <int DT, bool FLAT>
+__global__ __launch_bounds__(256) void checkpoint8_pack_kernel(const void* x, int64_t chunks, int64_t d, signed char* q, unsigned char* scales) {
+  constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;
+  const Checkpoint8Place p = checkpoint8_place<N, FLAT>((int64_t)blockIdx.x * 256 + threadIdx.x, chunks, d);
   float f[N];
-  widen_chunk<DT>(load_chunk<DT>((const char*)x + row * d * Chunk<DT>::BYTES, col, left), f);
-  const float m = checkpoint8_top<N, PER>(f);
-  if (left <= 0) return;
-  const int e = checkpoint8_exponent<DT>(m);
-  store_q<N>(q + row * d + col, left, f, power_of_two(-e));
-  if (c % PER == 0) scales[block] = (unsigned char)(e + 127);
+  widen_chunk<DT>(load_chunk<DT, FLAT>(x, p.at, p.left), f);
+  const uint32_t top = checkpoint8_top<N, PER>(f);
+  if (p.left <= 0) return;
+  const int e = checkpoint8_keep<DT>(q + p.at, p.left, f, top);
+  if ((threadIdx.x & (PER - 1)) == 0) scales[p.block] = (unsigned char)(e + 127);
 }
 
 // And back.
-template <int DT>
-__global__ __launch_bounds__(256) void checkpoint8_unpack_kernel(const signed char* q, const unsigned char* scales, int64_t rows, int64_t d, void* x) {
-  constexpr int N = Chunk<DT>::N, PER = CKPT8_BLOCK / N;
-  const int64_t nb = checkpoint8_blocks(d), chunks = rows * nb * PER;
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= chunks) return;
-  const int64_t block = c / PER, row = block / nb, b = block - row * nb;
-  const int64_t col = b * CKPT8_BLOCK + (c % PER) * N, left = d - col;
-  if (left <= 0) return;
+template <int DT, bool FLAT>
+__global__ __launch_bounds__(256) void checkpoint8_unpack_kernel(const signed char* q, const unsigned char* scales, int64_t chunks, int64_t d, void* x) {
+  constexpr int N = Chunk<DT>::N;
+  const Checkpoint8Place p = checkpoint8_place<N, FLAT>((int64_t)blockIdx.x * 256 + threadIdx.x, chunks, d);
+  if (p.left <= 0) return;
   uint32_t v[N / 4];
-  load_q<N>(q + row * d + col, left, v);
-  const float scale = power_of_two((int)scales[block] - 127);
+  load_q<N>(q + p.at, p.left, v);
   float f[N];
-  checkpoint8_values<N>(v, scale, f);
-  store_chunk<DT>((char*)x + row * d * Chunk<DT>::BYTES, col, left, round_chunk<DT>(f));
+  checkpoint8_values<N>(v, power_of_two((int)scales[p.block] - 127), f);
+  store_chunk<DT, FLAT>(x, p.at, p.left, round_chunk<DT>(f));
 }
 
 }  // namespace flashdp

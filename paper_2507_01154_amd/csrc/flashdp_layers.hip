@@ -180,11 +180,11 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   const bool held = p.columns <= NORM_LONG;
   p.col_tiles = held ? 1 : (p.columns + 255) / 256;
   p.token = held && T == 1;
-  // about two workgroups of 16 waves per compute unit, each going through its rows at least twice (a partial sum is written and read
-  // for every chunk of rows: 8 x 2048 x 5120 bf16, chunks of 16 rows 135 us, of 32 ...)
+  // about two times 16 waves per compute unit, every workgroup going through its rows at least twice, and no fewer than 16 tokens to a partial
+  // sum, below which writing and reading them shows
   const NormGradKernel kernel = held ? norm_grad_kernel_of(d, dtype, p.token) : NormGradKernel{nullptr, 256, 8};
-  const int64_t want = (2 * 256 * (1024 / kernel.threads) + B * p.col_tiles - 1) / (B * p.col_tiles);
-  const int64_t k = p.token ? 1 : std::max<int64_t>(1, std::min(want, (T + 2 * kernel.rows - 1) / (2 * kernel.rows)));
+  const int64_t want = (2 * 256 * (1024 / kernel.threads) + B * p.col_tiles - 1) / (B * p.col_tiles), fewest = std::max(2 * kernel.rows, 16);
+  const int64_t k = p.token ? 1 : std::max<int64_t>(1, std::min(want, (T + fewest - 1) / fewest));
   p.rows_per_chunk = (T + k - 1) / k;
   p.chunks = (T + p.rows_per_chunk - 1) / p.rows_per_chunk;
   return p;
@@ -438,6 +438,10 @@ int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, 
   return FLASHDP_OK;
 }
 
+// Chunks of 16 bytes that whole blocks of 32 features hold, and workgroups that go through them.
+static int64_t checkpoint8_chunks(int64_t rows, int64_t d, int dtype) { return rows * checkpoint8_blocks(d) * (CKPT8_BLOCK / chunk_elements(dtype)); }
+static int64_t checkpoint8_grid(int64_t chunks) { return (chunks + 255) / 256; }
+
 size_t flashdp_checkpoint8_bytes(int64_t rows, int64_t d) {
   if (check_rows(rows, d) != FLASHDP_OK) return 0;
   return (size_t)(checkpoint8_scales_at(rows, d) + rows * checkpoint8_blocks(d));
@@ -448,14 +452,16 @@ int flashdp_checkpoint8_pack(const void* X, int64_t rows, int64_t d, int dtype, 
   int st = check_rows(rows, d);
   if (st != FLASHDP_OK) return st;
   if (!aligned(X, 16) || !aligned(packed, 16)) return FLASHDP_MISALIGNED;
-  const int64_t grid = (rows * checkpoint8_blocks(d) * (CKPT8_BLOCK / chunk_elements(dtype)) + 255) / 256;
-  if (grid > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  const int64_t chunks = checkpoint8_chunks(rows, d, dtype);
+  if (checkpoint8_grid(chunks) > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
   int dev = 0;
   if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
   signed char* q = static_cast<signed char*>(packed);
   unsigned char* scales = static_cast<unsigned char*>(packed) + checkpoint8_scales_at(rows, d);
   HIP_TRY(by_dtype(dtype, [&](auto dt) {
-    return launch(checkpoint8_pack_kernel<decltype(dt)::value>, grid, 256, 0, static_cast<hipStream_t>(stream), X, rows, d, q, scales);
+    constexpr int DT = decltype(dt)::value;
+    return launch(d % CKPT8_BLOCK == 0 ? checkpoint8_pack_kernel<DT, true> : checkpoint8_pack_kernel<DT, false>, checkpoint8_grid(chunks), 256, 0,
+                  static_cast<hipStream_t>(stream), X, chunks, d, q, scales);
   }));
   return FLASHDP_OK;
 }
@@ -465,14 +471,16 @@ int flashdp_checkpoint8_unpack(const void* packed, int64_t rows, int64_t d, int 
   int st = check_rows(rows, d);
   if (st != FLASHDP_OK) return st;
   if (!aligned(X, 16) || !aligned(packed, 16)) return FLASHDP_MISALIGNED;
-  const int64_t grid = (rows * checkpoint8_blocks(d) * (CKPT8_BLOCK / chunk_elements(dtype)) + 255) / 256;
-  if (grid > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
+  const int64_t chunks = checkpoint8_chunks(rows, d, dtype);
+  if (checkpoint8_grid(chunks) > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
   int dev = 0;
   if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
   const signed char* q = static_cast<const signed char*>(packed);
   const unsigned char* scales = static_cast<const unsigned char*>(packed) + checkpoint8_scales_at(rows, d);
   HIP_TRY(by_dtype(dtype, [&](auto dt) {
-    return launch(checkpoint8_unpack_kernel<decltype(dt)::value>, grid, 256, 0, static_cast<hipStream_t>(stream), q, scales, rows, d, X);
+    constexpr int DT = decltype(dt)::value;
+    return launch(d % CKPT8_BLOCK == 0 ? checkpoint8_unpack_kernel<DT, true> : checkpoint8_unpack_kernel<DT, false>, checkpoint8_grid(chunks), 256, 0,
+                  static_cast<hipStream_t>(stream), q, scales, chunks, d, X);
   }));
   return FLASHDP_OK;
 }

@@ -76,10 +76,14 @@ __device__ __forceinline__ void finish_chunk(const ForwardArgs& a, int64_t at, i
   if (a.keep == KEEP_EIGHT) {
     float there[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) there[k] = k < left ? z[k] : 0.0f;
-    const int e = checkpoint8_exponent<DT>(checkpoint8_top<N, PER>(there));
+    for (int k = 0; k < N; ++k) there[k] = z[k];
+    if (left < N) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) there[k] = k < left ? z[k] : 0.0f;
+    }
+    const uint32_t top = checkpoint8_top<N, PER>(there);
     if (left > 0) {
-      store_q<N>((signed char*)a.Z + at, left, z, power_of_two(-e));
+      const int e = checkpoint8_keep<DT>((signed char*)a.Z + at, left, z, top);
       if ((threadIdx.x & (PER - 1)) == 0) a.scales[block] = (unsigned char)(e + 127);
     }
   }
