@@ -61,9 +61,10 @@
  *                                256x256 with 32-deep k-tiles - these three stage tiles through registers -,
  *                                256x256, 384x192, 192x384 with 32-deep k-tiles loaded straight into LDS);
  *                                -1 sends fp32 inputs and sizes that are no multiples of 8 to the generic kernel;
- *   FLASHDP_FORWARD = 0 .. 9     forces the kernel of flashdp_linear_forward where the shape allows it: direct-to-LDS tiles of 16 x 16, 16 x 32,
+ *   FLASHDP_FORWARD = 0 .. 11    forces the kernel of flashdp_linear_forward where the shape allows it: direct-to-LDS tiles of 16 x 16, 16 x 32,
  *                                32 x 32, 64 x 64, 128 x 128, 128 x 128 with two workgroups per CU, 256 x 256 (0 .. 6, d_in * size a
  *                                multiple of 16 bytes); few rows, 64 x 64 and 128 x 128 tiles through registers (7 .. 9, other d_in);
+ *                                fp32 in bfloat16 parts on tiles of 128 x 256 and 64 x 128 (10, 11);
  *   FLASHDP_OVERLAP_GRID = n     workgroups of the aggregation kernel in the overlapped schedule (default: one per
  *                                compute unit).
  */
@@ -254,7 +255,8 @@ enum { FLASHDP_ACT_NONE = 0, FLASHDP_ACT_RELU = 1, FLASHDP_ACT_GELU = 2, FLASHDP
  * Z, if not NULL, receives what the backward pass of the activation needs: [rows][d_out] in `dtype` (z_8bit = 0), or an 8-bit checkpoint of
  * flashdp_checkpoint8_bytes(rows, d_out) bytes made from the fp32 sums (z_8bit = 1).  The activation is taken of the fp32 sum,
  * not of the kept Z.  Y may be residual; it may overlap nothing else.  Rows are independent of each other to the bit only among calls
- * of the same number of rows (the order of additions goes by the sizes).  No workspace. */
+ * of the same number of rows (the order of additions goes by the sizes).  fp32 products of d_in >= 64 may be formed from operands cut into three
+ * bfloat16 parts (error below that of the fp32 sums), where an operand that is infinite counts as NaN.  No workspace. */
 int flashdp_linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t rows, int64_t d_in, int64_t d_out,
                            int dtype, int activation, void* Y, void* Z, int z_8bit, void* stream);
 

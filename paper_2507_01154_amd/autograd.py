@@ -13,6 +13,7 @@ batch dimension is the first one and everything between it and the feature dimen
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as F
 
@@ -151,6 +152,7 @@ class _DPLinearEpilogueFn(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         kept, z, weight = ctx.saved_tensors
         module, seed, norms, bias_norms, B, T, eight, act, C, bias_C, sigma, layer, schedule, add_noise = ctx.cfg
@@ -278,6 +280,7 @@ class _DPLayerNormFn(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         xs, weight, mean, rstd = ctx.saved_tensors
         module, seed, norms, B, T, has_bias, C, sigma, layer, add_noise = ctx.cfg

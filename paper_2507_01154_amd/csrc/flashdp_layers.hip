@@ -14,6 +14,7 @@
 #include "forward_deep.hip.h"
 #include "forward_large.hip.h"
 #include "forward_rows.hip.h"
+#include "forward_split.hip.h"
 #include "forward_tile.hip.h"
 #include "layernorm.hip.h"
 #include "vector_dp.hip.h"
@@ -194,25 +195,32 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
 
 // Which kernel forms a product.  For rows of whole 16-byte chunks a ladder of tiles; a call takes the one whose rounds are
 // the shortest.  A round of `per_cu` workgroups on every compute unit takes start + tile * (k-tiles of 128 bytes) microseconds, one
-// of at most one workgroup per unit start + alone * k-tiles (fitted to 150 products of one to 8192 rows, 768 to 13824 features; 16-bit types,
-// then fp32, whose k-tiles are half as deep and bound by the matrix cores from 64 x 64 on).  us, in the order of the ladder (- = not tried):
+// of at most one workgroup per unit start + alone * k-tiles, and epilogue more where the epilogue has an activation or 8-bit sums (fitted to 170
+// products of one to 8192 rows, 768 to 13824 features; 16-bit types, then fp32, whose k-tiles are half as deep).  us, tiles of 16 x 16, 16 x 32, 32 x 32,
+// 64 x 64, 128 x 128, 128 x 128 with two workgroups per unit, 256 x 256 (- = not tried):
 // bf16 1 x 4096 -> 4096: 7.2, 10.0, 10.0, 14.7, 34, -, -; fp16 8 x 768 -> 50257: 23.3, 16.6, 18.4, 22.4, -, -, -; bf16 128 x 4096 -> 4096: -, -, 14.6, 15.2, 34.9, 46, 74;
-// epilogue: microseconds that an activation or 8-bit sums add to a round (8192 x 768 -> 3072 with GELU and both: -, -, -, 127, 80, 62, 69 beside
-// 109, 62, 51, 51 without).  256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
-// bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; fp32 128 x 4096 -> 4096: -, -, 45, 74, 257, 247, -; 2048 x 4096 -> 4096: -, -, 665, 588, 520, 480, 931.
+// 256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
+// bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; 8192 x 768 -> 3072: -, -, 167, 109, 62, 51, 51, with GELU and Z in 8 bits -, -, -, 127, 80, 62, 69.
+// fp32, 32 x 32, 64 x 64, 128 x 128 twice, then in bfloat16 parts on 64 x 128 and 128 x 256: 128 x 4096 -> 4096: 48, 74, 247, 127, 267; 512 x 4096 -> 4096: 169,
+// 148, 249, 142, 273; 2048 x 4096 -> 4096: 663, 586, 478, 385, 303; 8192 x 768 -> 3072: 429, 382, 286, 228, 194.  Relative errors in norm there, fp32
+// instruction and parts: 1.15e-6, 1.02e-6; K = 768: 5.0e-7, 4.4e-7.
 // Rows that no 16-byte chunks divide: direct loads to LDS need 4-byte alignment; few rows take the kernel that reads W straight into
-// registers, others tiles staged through registers (bf16 64 x 4096 -> 4096: 23.8, 39.5).
-enum ForwardPath { FWD_16x16 = 0, FWD_16x32, FWD_32x32, FWD_64x64, FWD_128x128, FWD_128x128_TWO, FWD_256x256, FWD_LADDER, FWD_ROWS = FWD_LADDER, FWD_ANY_64, FWD_ANY_128, FWD_PATHS };
-struct ForwardRung { int bm, bn, per_cu; double start, tile, alone, tile32, alone32, epilogue; };   // tile32 = 0: not for fp32
-constexpr ForwardRung FORWARD_LADDER[FWD_LADDER] = {
-    {16, 16, 2, 1.9, 0.115, 0.085, 0.115, 0.09, 0.2}, {16, 32, 3, 2.0, 0.15, 0.12, 0.3, 0.21, 0.3}, {32, 32, 2, 1.6, 0.18, 0.1, 0.34, 0.2, 0.4},
-    {64, 64, 1, 2.6, 0.19, 0.19, 0.56, 0.56, 0.7},    {128, 128, 1, 4.0, 0.54, 0.54, 0.0, 0.0, 2.9}, {128, 128, 2, 6.6, 0.87, 0.65, 3.7, 1.92, 3.7},
-    {256, 256, 1, 7.0, 1.54, 1.54, 0.0, 0.0, 9.0}};
+// registers, others tiles staged through registers (bf16 64 x 4096 -> 4096: 23.8, 39.5), fp32 the parts where they are faster
+// (1024 x 1001 -> 2304: 71, 57).
+enum ForwardPath { FWD_16x16 = 0, FWD_16x32, FWD_32x32, FWD_64x64, FWD_128x128, FWD_128x128_TWO, FWD_256x256, FWD_ROWS, FWD_ANY_64, FWD_ANY_128, FWD_SPLIT, FWD_SPLIT_SMALL, FWD_PATHS };
+struct ForwardCost { double start, tile, alone; };
+struct ForwardRung { ForwardPath path; int bm, bn, per_cu; ForwardCost bits16, bits32; double epilogue; bool direct; };   // no tile: not for that type
+constexpr ForwardRung FORWARD_LADDER[] = {
+    {FWD_16x16, 16, 16, 2, {1.9, 0.115, 0.085}, {1.9, 0.115, 0.09}, 0.2, true},   {FWD_16x32, 16, 32, 3, {2.0, 0.15, 0.12}, {2.0, 0.3, 0.21}, 0.3, true},
+    {FWD_32x32, 32, 32, 2, {1.6, 0.18, 0.1}, {1.6, 0.34, 0.2}, 0.4, true},        {FWD_64x64, 64, 64, 1, {2.6, 0.19, 0.19}, {2.6, 0.56, 0.56}, 0.7, true},
+    {FWD_128x128, 128, 128, 1, {4.0, 0.54, 0.54}, {}, 2.9, true},                 {FWD_128x128_TWO, 128, 128, 2, {6.6, 0.87, 0.65}, {6.6, 3.7, 1.92}, 3.7, true},
+    {FWD_256x256, 256, 256, 1, {7.0, 1.54, 1.54}, {}, 9.0, true},                 {FWD_SPLIT, 128, 256, 1, {}, {9.5, 2.32, 2.02}, 4.5, false},
+    {FWD_SPLIT_SMALL, 64, 128, 2, {}, {5.6, 1.45, 0.95}, 2.0, false}};
+constexpr int64_t SPLIT_LEAST = 64;   // fewest products of a sum formed from parts: their error is allowed from there on (forward_split.hip.h)
 
-bool forward_direct(int64_t d_in, int dtype) {
-  const int64_t kb = d_in * (dtype == FLASHDP_F32 ? 4 : 2);
-  return kb % 16 == 0 && kb < (int64_t(1) << 23) - 4096;      // 256 rows lie within the 2 GiB that a buffer descriptor reaches
-}
+bool forward_direct(int64_t d_in, int dtype) { return d_in * (dtype == FLASHDP_F32 ? 4 : 2) % 16 == 0; }
+// 256 rows lie within the 2 GiB that a buffer descriptor reaches
+bool forward_described(int64_t d_in, int dtype) { return d_in * (dtype == FLASHDP_F32 ? 4 : 2) < (int64_t(1) << 23) - 4096; }
 // tiles of a rung, or -1 where they are too many for a grid
 int64_t forward_tiles(int64_t rows, int64_t d_out, int bm, int bn) {
   const int64_t tm = (rows + bm - 1) / bm, tn = (d_out + bn - 1) / bn;
@@ -222,26 +230,31 @@ int64_t forward_tiles(int64_t rows, int64_t d_out, int bm, int bn) {
 // blocks_of_32: Z goes out in 8 bits; busy: the epilogue has more to do than to round and store.
 ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, bool blocks_of_32, bool busy) {
   const int forced = api::forward_override();
-  if (!forward_direct(d_in, dtype)) {
-    if (forced == FWD_ROWS || forced == FWD_ANY_64 || forced == FWD_ANY_128) return forced == FWD_ROWS && rows > 64 ? FWD_ANY_64 : (ForwardPath)forced;
-    return rows <= 64 ? FWD_ROWS : forward_tiles(rows, d_out, 128, 128) < 256 && forward_tiles(rows, d_out, 64, 64) >= 0 ? FWD_ANY_64 : FWD_ANY_128;
-  }
-  const int64_t cus = api::compute_units(), nk = (d_in * (dtype == FLASHDP_F32 ? 4 : 2) + 127) / 128;
-  int best = -1;
+  const bool f32 = dtype == FLASHDP_F32, described = forward_described(d_in, dtype), direct = described && forward_direct(d_in, dtype);
+  if (!direct && rows <= 64 && (forced < FWD_ANY_64 || forced >= FWD_PATHS)) return FWD_ROWS;
+  const int64_t cus = api::compute_units(), nk = (d_in * (f32 ? 4 : 2) + 127) / 128;
+  ForwardPath best = FWD_PATHS;
   double least = 0.0;
-  for (int r = 0; r < FWD_LADDER; ++r) {
-    const ForwardRung& g = FORWARD_LADDER[r];
-    if ((blocks_of_32 && g.bn % CKPT8_BLOCK != 0) || (dtype == FLASHDP_F32 && g.tile32 == 0.0)) continue;
-    const int64_t tiles = forward_tiles(rows, d_out, g.bm, g.bn);
-    if (tiles < 0) continue;
-    if (forced == r) return (ForwardPath)r;
-    const int64_t slots = cus * g.per_cu, rest = tiles % slots;
-    const double tile = dtype == FLASHDP_F32 ? g.tile32 : g.tile, alone = dtype == FLASHDP_F32 ? g.alone32 : g.alone;
-    const double start = g.start + (busy ? g.epilogue : 0.0);
-    const double t = (double)(tiles / slots) * (start + tile * nk) + (rest == 0 ? 0.0 : start + (rest <= cus ? alone : tile) * nk);
-    if (best < 0 || t < least) { best = r; least = t; }
+  auto offer = [&](ForwardPath path, int64_t tiles, int per_cu, const ForwardCost& c, double epilogue) {
+    const int64_t slots = cus * per_cu, rest = tiles % slots;
+    const double start = c.start + (busy ? epilogue : 0.0);
+    double t = (double)(tiles / slots) * (start + c.tile * nk) + (rest == 0 ? 0.0 : start + (rest <= cus ? c.alone : c.tile) * nk);
+    if (forced == path) t = -1.0;
+    if (best == FWD_PATHS || t < least) { best = path; least = t; }
+  };
+  if (!direct) {
+    const int64_t t64 = forward_tiles(rows, d_out, 64, 64), t128 = forward_tiles(rows, d_out, 128, 128);
+    const bool small = forced == FWD_ANY_64 || (forced != FWD_ANY_128 && t128 < 256);
+    if (small && t64 >= 0) offer(FWD_ANY_64, t64, 4, f32 ? ForwardCost{3.0, 2.2, 0.83} : ForwardCost{3.0, 1.0, 0.57}, 0.0);
+    else if (t128 >= 0) offer(FWD_ANY_128, t128, 2, f32 ? ForwardCost{6.6, 4.4, 2.2} : ForwardCost{6.6, 1.28, 0.9}, 0.0);
   }
-  return best < 0 ? FWD_PATHS : (ForwardPath)best;
+  for (const ForwardRung& g : FORWARD_LADDER) {
+    const ForwardCost& c = f32 ? g.bits32 : g.bits16;
+    if (c.tile == 0.0 || (g.direct ? !direct : !described || (d_in < SPLIT_LEAST && forced != g.path)) || (blocks_of_32 && g.bn % CKPT8_BLOCK != 0)) continue;
+    const int64_t tiles = forward_tiles(rows, d_out, g.bm, g.bn);
+    if (tiles >= 0) offer(g.path, tiles, g.per_cu, c, g.epilogue);
+  }
+  return best;
 }
 
 template <typename Cfg>
@@ -266,6 +279,13 @@ using Deep32x32 = ForwardDeepCfg<32, 32, 4, 1, 8, 2>;
 using Deep64x64 = ForwardDeepCfg<64, 64, 4, 2, 8, 2>;
 using Deep128x128 = ForwardDeepCfg<128, 128, 2, 4, 4, 1>;
 
+using Split128x256 = ForwardSplitCfg<128, 256, 2, 4>;
+using Split64x128 = ForwardSplitCfg<64, 128, 2, 2>;
+template <typename Cfg>
+hipError_t launch_forward_split(ForwardArgs& a, hipStream_t st) {
+  return launch_forward_tiles<Cfg>(a.K % 4 == 0 ? forward_split_kernel<Cfg, false> : forward_split_kernel<Cfg, true>, a, st);
+}
+
 template <int DT>
 hipError_t run_forward(ForwardPath path, ForwardArgs& a, hipStream_t st) {
   switch (path) {
@@ -280,6 +300,8 @@ hipError_t run_forward(ForwardPath path, ForwardArgs& a, hipStream_t st) {
       if (a.rows <= 16) return launch_forward_rows<ForwardRowsCfg<2, 1, 8>, DT>(a, st);
       if (a.rows <= 32) return launch_forward_rows<ForwardRowsCfg<2, 2, 8>, DT>(a, st);
       return launch_forward_rows<ForwardRowsCfg<2, 4, 8>, DT>(a, st);
+    case FWD_SPLIT: if constexpr (DT == DT_F32) return launch_forward_split<Split128x256>(a, st); else return hipErrorInvalidValue;
+    case FWD_SPLIT_SMALL: if constexpr (DT == DT_F32) return launch_forward_split<Split64x128>(a, st); else return hipErrorInvalidValue;
     case FWD_ANY_64: return launch_forward_tiles<ForwardTileCfg<64, 64>>(forward_tile_kernel<ForwardTileCfg<64, 64>, DT>, a, st);
     case FWD_ANY_128: return launch_forward_tiles<ForwardTileCfg<128, 128>>(forward_tile_kernel<ForwardTileCfg<128, 128>, DT>, a, st);
     default: return hipErrorInvalidValue;
@@ -288,6 +310,7 @@ hipError_t run_forward(ForwardPath path, ForwardArgs& a, hipStream_t st) {
 
 const char* forward_kernel_name(ForwardPath path) {
   return path == FWD_ROWS ? "forward_rows_kernel" : path == FWD_ANY_64 || path == FWD_ANY_128 ? "forward_tile_kernel"
+         : path == FWD_SPLIT || path == FWD_SPLIT_SMALL ? "forward_split_kernel"
          : path == FWD_128x128_TWO || path == FWD_256x256 ? "forward_large_kernel" : "forward_deep_kernel";
 }
 
@@ -302,8 +325,7 @@ int flashdp_linear_forward(const void* X, const void* W, const void* bias, const
   if (st == FLASHDP_OK) st = check_rows(rows, d_out);
   if (st != FLASHDP_OK) return st;
   const ForwardPath path = forward_path(rows, d_in, d_out, dtype, z_8bit != 0, activation != FLASHDP_ACT_NONE || z_8bit != 0);
-  if (path == FWD_PATHS || (path >= FWD_ANY_64 && forward_tiles(rows, d_out, path == FWD_ANY_64 ? 64 : 128, path == FWD_ANY_64 ? 64 : 128) < 0))
-    return FLASHDP_UNSUPPORTED_SHAPE;    // more tiles than a grid holds
+  if (path == FWD_PATHS) return FLASHDP_UNSUPPORTED_SHAPE;    // more tiles than a grid holds
   if (!aligned(X, 16) || !aligned(W, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(Z, 16)) return FLASHDP_MISALIGNED;
   int dev = 0;
   if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;

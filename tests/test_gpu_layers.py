@@ -160,10 +160,11 @@ def test_forward_epilogues(rows, act, dtype):
     check_forward(rows, 136, 200, dtype, act, True, True, None, seed=30, inplace=True)      # added to the residual in place
 
 
-# the kernels of the ladder (0 to 6: rows of whole 16-byte chunks; 4 and 6 are not made for fp32) and those for other rows (7 to 9), on sizes that
-# leave them ragged edges, one k-tile and many, and more k-tiles than stages
+# the kernels of the ladder (0 to 6: rows of whole 16-byte chunks; 4 and 6 are not made for fp32), those for other rows (7 to 9) and those of fp32
+# in bfloat16 parts (10, 11), on sizes that leave them ragged edges, one k-tile and many, and more k-tiles than stages
 FORCED = [(k, r, K, D) for k in range(7) for r, K, D in [(1, 8, 8), (5, 64, 40), (33, 136, 72), (70, 1160, 136), (300, 520, 328)]] + \
-         [(k, r, K, D) for k in (7, 8, 9) for r, K, D in [(1, 1, 8), (5, 63, 40), (33, 137, 75), (64, 1161, 137), (150, 517, 329)]]
+         [(k, r, K, D) for k in (7, 8, 9) for r, K, D in [(1, 1, 8), (5, 63, 40), (33, 137, 75), (64, 1161, 137), (150, 517, 329)]] + \
+         [(k, r, K, D) for k in (10, 11) for r, K, D in [(1, 64, 8), (70, 1161, 137), (300, 520, 328), (150, 66, 600)]]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "fp32"])
@@ -174,8 +175,8 @@ def test_every_forward_kernel(kernel, rows, K, D, dtype):
         check_forward(rows, K, D, dtype, "gelu", True, True, "dtype", seed=50)
         check_forward(rows, K, D, dtype, "silu", True, False, "8bit", seed=60)
         want = {7: "forward_rows_kernel" if rows <= 64 else "forward_tile_kernel", 8: "forward_tile_kernel", 9: "forward_tile_kernel",
-                5: "forward_large_kernel", 6: "forward_large_kernel"}.get(kernel, "forward_deep_kernel")
-        if dtype != "fp32" or kernel not in (4, 6):
+                5: "forward_large_kernel", 6: "forward_large_kernel", 10: "forward_split_kernel", 11: "forward_split_kernel"}.get(kernel, "forward_deep_kernel")
+        if (kernel < 10 and dtype != "fp32") or (kernel not in (4, 6) and dtype == "fp32"):
             assert F.flashdp_last_kernel() == want or kernel == 0           # (8-bit blocks of 32 features are wider than the smallest tile)
 
 
@@ -196,6 +197,30 @@ def test_forward_large(rows, K, D, dtype):
     within(yc, y64, (1 + h) * (1.13 * slack + 2.0 ** -19 * z64.abs().clamp(min=1) + 2 * U * y64.abs()) + h * y64.abs() + tiny, "y")
     # bounds of the worst case are loose by sqrt(K): the error in norm is that of one rounding, fp32 sums beside it
     assert float((yc - y64).norm() / y64.norm()) <= h + 2 * math.sqrt(K) * U
+
+
+@pytest.mark.parametrize("kernel", [10, 11])
+def test_parts_of_floats_over_the_range_of_their_exponents(kernel):
+    """fp32 in bfloat16 parts: rows of X scaled from 2^-100 to 2^100 (down to where the third part is a normal number), values with all 24 bits
+    set, powers of two, the largest number, and rows that are not finite, which spoil themselves alone."""
+    rows, K, D = 40, 136, 72
+    x, w = rand(1, (rows, K), "fp32"), rand(2, (D, K), "fp32")
+    x *= torch.logspace(-100, 100, rows, base=2)[:, None]
+    x[3], x[4] = float(2 ** 24 - 1), 2.0 ** torch.arange(-60, 76).float()
+    x[5] = 0.0
+    x[5, 0] = torch.finfo(torch.float32).max
+    x[6, 1], x[7, 2] = math.nan, math.inf
+    with env(FLASHDP_FORWARD=kernel):
+        y, _ = run_forward(x, w * 0.5, None, None, None, "fp32")
+        assert F.flashdp_last_kernel() == "forward_split_kernel"
+    x64, w64 = x.double(), w.double() * 0.5
+    fine = torch.ones(rows, dtype=torch.bool)
+    fine[6:8] = False
+    y64, mag = (x64 @ w64.T)[fine], (x64[fine].abs() @ w64.abs().T)
+    assert not torch.isfinite(y[~fine]).any()
+    got = y[fine]
+    over = y64.abs() > 3.4e38
+    within(got[~over], y64[~over], ((K + 2) * U * mag + 1e-45)[~over])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "fp32"])
@@ -403,6 +428,11 @@ def check_norm(B, T, d, dtype, bias=True, C=1.0, sigma=0.0, offset=0.5, inplace=
     gw, ew = per(dy64 * xh), per(dy64.abs() * exh) + (T + 3) * U * per((dy64 * xh).abs())
     G, err = (torch.cat((gw, per(dy64)), 1), torch.cat((ew, (T + 3) * U * per(dy64.abs())), 1)) if bias else (gw, ew)
     check_vector(g.cpu().reshape(-1), n.cpu(), G, err, C, sigma, 11, 2, F.FIELD_NORM)
+    if inplace:      # Y over X, too
+        over = Out((rows, d), f)
+        over.t.copy_(xd)
+        F.flashdp_layernorm_forward(over.t, wd, None if b is None else b.to(DEV), rows, d, CODE[dtype], eps, over.t)
+        assert torch.equal(over.cpu(), y.cpu())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "fp32"])
