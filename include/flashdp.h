@@ -233,11 +233,12 @@ int64_t flashdp_last_chunk(void);
  * backward pass of its activation and the DP gradients of biases and normalisations, and activations kept in 8 bits.  The
  * conventions above hold (device pointers, 16-byte aligned, rows one after the other, work enqueued on `stream`, argument errors
  * before anything is enqueued), with these additions:
- *   - any positive sizes are accepted, d_in, d_out and d up to 2^30, rows (B * T) below 2^40; rows need no alignment of their own;
+ *   - any positive sizes are accepted, d_in, d_out and d up to 2^30, rows (B * T) below 2^40 and 2^58 elements; rows need
+ *     no alignment of their own;
  *   - parameters (W, bias, gamma, beta) and activations have the type `dtype`; arithmetic is fp32, results are rounded once;
  *   - optional pointers may be NULL;
- *   - a workspace argument works as for flashdp_block_dp_grad: NULL takes the library-owned one, which is not grown
- *     while `stream` is being captured (FLASHDP_WORKSPACE_TOO_SMALL instead).
+ *   - a workspace argument works as for flashdp_block_dp_grad: NULL takes the library-owned one - but not while `stream` is being
+ *     captured (FLASHDP_WORKSPACE_TOO_SMALL instead): a later call that grows it would leave the graph with freed memory.
  *
  * DP gradients of a vector of parameters v (a bias; gamma and beta of a normalisation, which are one vector gamma, beta):
  *     g_i = sum_t dv_it     n_i = ||g_i||_2     out_grad = sum_i g_i / max(1, n_i / C) + sigma * C * z

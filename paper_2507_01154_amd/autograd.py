@@ -49,7 +49,7 @@ class deferred_weight_grads:
         for rec in self.pending:
             groups.setdefault((rec["B"], rec["T"], rec["dY"].dtype, rec["packed"]), []).append(rec)
         for (B, T, _, packed), recs in groups.items():
-            grad = F.flashdp_block_dp_grad_checkpoint8 if packed else F.flashdp_block_dp_grad_micro
+            grad = _grad_call(packed, packed)
             layers = []
             for r in recs:
                 r["out"] = torch.empty(r["weight"].shape, dtype=torch.float32, device=r["X"].device)
@@ -68,7 +68,21 @@ class deferred_weight_grads:
         self.pending = []
 
 
-def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module):
+def _grad_call(packed, room):
+    """The block call for activations as they are, or for 8-bit checkpoints of them.  Both take the library's workspace; with `room`, while a
+    graph is being captured, one of torch's, which the graph keeps."""
+    grad, size = ((F.flashdp_block_dp_grad_checkpoint8, F.flashdp_workspace_bytes_checkpoint8) if packed
+                  else (F.flashdp_block_dp_grad_micro, F.flashdp_workspace_bytes))
+    if not room or not torch.cuda.is_current_stream_capturing():
+        return grad
+
+    def call(layers, B, T, dtype, schedule, **kw):
+        grad(layers, B, T, dtype, schedule, _workspace(size(layers, B, T, dtype, schedule), layers[0]["X"].device), **kw)
+
+    return call
+
+
+def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module, room=False):
     """The weight's gradient, now or - inside deferred_weight_grads, where None is returned - in the block call at its end.  X is the
     activation [B, T, d_in], or with `packed` its 8-bit checkpoint."""
     pending = deferred_weight_grads._active
@@ -79,8 +93,7 @@ def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, n
     d_out, d_in = weight.shape
     grad_w = torch.empty((d_out, d_in), dtype=torch.float32, device=dY.device)
     L = [dict(X=X, dY=dY, d_in=d_in, d_out=d_out, C=C, sigma=sigma, seed=seed, layer=layer, out_grad=grad_w, out_norms=norms)]
-    grad = F.flashdp_block_dp_grad_checkpoint8 if packed else F.flashdp_block_dp_grad_micro
-    grad(L, B, T, F.dtype_code(dY), schedule, accumulate=False, add_noise=add_noise)
+    _grad_call(packed, room)(L, B, T, F.dtype_code(dY), schedule, accumulate=False, add_noise=add_noise)
     if module is not None and module.keep_fp32_grad:
         module.grad_fp32 = grad_w.clone() if module.grad_fp32 is None else module.grad_fp32 + grad_w
     return grad_w.to(weight.dtype)
@@ -126,6 +139,8 @@ class _DPLinearEpilogueFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, module, seed, norms, bias_norms, grad_mode):
         d_out, d_in = weight.shape
+        if x.dim() < 2 or x.shape[-1] != d_in:
+            raise TypeError(f"the input is [samples, ..., {d_in}], not {tuple(x.shape)}")
         if x.dtype != weight.dtype or (residual is not None and (residual.dtype != x.dtype or residual.shape != (*x.shape[:-1], d_out))):
             raise TypeError("input, weight and residual need one dtype, and the residual the output's shape")
         xs = _dense(x)
@@ -178,7 +193,7 @@ class _DPLinearEpilogueFn(torch.autograd.Function):
                 grad_x = torch.matmul(dz, weight)
             if need_w:
                 grad_w = _weight_grad(kept if eight else kept.reshape(B, T, d_in), eight, dz.reshape(B, T, d_out), B, T, weight, float(C), float(sigma),
-                                      seed, layer, schedule, norms, add_noise, module)
+                                      seed, layer, schedule, norms, add_noise, module, room=True)
         return grad_x, grad_w, grad_b, dy if need_r else None, None, None, None, None, None
 
 
@@ -265,8 +280,8 @@ class DPLinear(_DPModule):
 class _DPLayerNormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, module, seed, norms):
-        if x.dtype != weight.dtype or x.shape[-1] != weight.shape[0]:
-            raise TypeError("input and weight need one dtype, and the input's last dimension the weight's size")
+        if x.dim() < 2 or x.dtype != weight.dtype or x.shape[-1] != weight.shape[0]:
+            raise TypeError("input and weight need one dtype, and the input is [samples, ..., the weight's size]")
         d = weight.shape[0]
         xs = _dense(x)
         rows, code = xs.numel() // d, F.dtype_code(xs)

@@ -330,29 +330,31 @@ def _float_type(dtype: int):
     return _FLOATS.get(dtype)
 
 
-def _buffer(t, n: int, dtype, where: str) -> Optional[int]:
-    """Address of a tensor that a call uses as a buffer of n elements: rows lie one after the other, and the type is
+def _buffer(t, n: int, dtype, where: str, device: int) -> Optional[int]:
+    """Address of a tensor that a call uses as a buffer of n elements on its device: rows lie one after the other, and the type is
     the call's.  (A view with strides of its own, or a shorter one, would be read and written past its end.)"""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < n or not t.is_cuda:
-        raise FlashDPError(INVALID_ARGUMENT, f"{where}: a contiguous device tensor of {dtype} with {n} elements is needed, "
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < n or t.get_device() != device:
+        raise FlashDPError(INVALID_ARGUMENT, f"{where}: a contiguous tensor of {dtype} with {n} elements on device {device} is needed, "
                                              f"not {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _here(t, stream, where: str) -> Optional[int]:
-    """Handle of the stream to enqueue on.  The library works on the current device; so has the caller's tensor to be."""
+def _here(t, stream, where: str):
+    """Handle of the stream to enqueue on, and the device.  The library works on the current device; so has the caller's tensor to be."""
     device = t.get_device()
     if device < 0 or device != _torch.cuda.current_device():
         raise FlashDPError(INVALID_ARGUMENT, f"{where}: the tensors are on {t.device}, which is not the current device")
     if stream is None:
-        return _torch._C._cuda_getCurrentRawStream(device) or None      # (torch.cuda.current_stream() makes an object, a microsecond)
-    return _stream_handle(stream)
+        return _torch._C._cuda_getCurrentRawStream(device) or None, device      # (torch.cuda.current_stream() makes an object, a microsecond)
+    return _stream_handle(stream), device
 
 
-def _room(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+def _room(workspace, where: str, device: int):
+    if workspace is None:
+        return None, 0
+    return _buffer(workspace, 0, workspace.dtype, where, device), workspace.numel() * workspace.element_size()
 
 
 def flashdp_linear_forward(X, W, bias, residual, rows: int, d_in: int, d_out: int, dtype: int, activation, Y, Z=None, z_8bit: bool = False,
@@ -360,11 +362,11 @@ def flashdp_linear_forward(X, W, bias, residual, rows: int, d_in: int, d_out: in
     """Y = act(X W^T + bias) + residual; Z, if given, receives X W^T + bias, in the call's type or as an 8-bit checkpoint (a uint8
     tensor of flashdp_checkpoint8_bytes(rows, d_out)).  activation: a name or code."""
     w, f = "flashdp_linear_forward", _float_type(dtype)
-    st = _here(X, stream, w)
-    z = _buffer(Z, flashdp_checkpoint8_bytes(rows, d_out), _torch.uint8, w) if z_8bit else _buffer(Z, rows * d_out, f, w)
-    _check(lib().flashdp_linear_forward(_buffer(X, rows * d_in, f, w), _buffer(W, d_out * d_in, f, w), _buffer(bias, d_out, f, w),
-                                        _buffer(residual, rows * d_out, f, w), rows, d_in, d_out, int(dtype), activation_code(activation),
-                                        _buffer(Y, rows * d_out, f, w), z, int(bool(z_8bit)), st), w)
+    st, dev = _here(X, stream, w)
+    z = _buffer(Z, flashdp_checkpoint8_bytes(rows, d_out), _torch.uint8, w, dev) if z_8bit else _buffer(Z, rows * d_out, f, w, dev)
+    _check(lib().flashdp_linear_forward(_buffer(X, rows * d_in, f, w, dev), _buffer(W, d_out * d_in, f, w, dev), _buffer(bias, d_out, f, w, dev),
+                                        _buffer(residual, rows * d_out, f, w, dev), rows, d_in, d_out, int(dtype), activation_code(activation),
+                                        _buffer(Y, rows * d_out, f, w, dev), z, int(bool(z_8bit)), st), w)
 
 
 def flashdp_activation_workspace_bytes(B: int, T: int, d_out: int, dtype: int) -> int:
@@ -375,20 +377,20 @@ def flashdp_activation_dp_grad(dY, Z, z_8bit: bool, B: int, T: int, d_out: int, 
                                dZ, out_grad, out_norms=None, workspace=None, stream=None, accumulate: bool = False, add_noise: bool = True):
     """dZ = dY act'(Z) and the clipped, noised gradient of the bias (out_grad [d_out] fp32, or None)."""
     w, f, n = "flashdp_activation_dp_grad", _float_type(dtype), B * T * d_out
-    st = _here(dY, stream, w)
-    z = _buffer(Z, flashdp_checkpoint8_bytes(B * T, d_out), _torch.uint8, w) if z_8bit else _buffer(Z, n, f, w)
-    ws, ws_bytes = _room(workspace)
-    _check(lib().flashdp_activation_dp_grad(_buffer(dY, n, f, w), z, int(bool(z_8bit)), B, T, d_out, int(dtype), activation_code(activation), C, sigma, seed, layer,
-                                            _buffer(dZ, n, f, w), _buffer(out_grad, d_out, _torch.float32, w), _buffer(out_norms, B, _torch.float32, w),
+    st, dev = _here(dY, stream, w)
+    z = _buffer(Z, flashdp_checkpoint8_bytes(B * T, d_out), _torch.uint8, w, dev) if z_8bit else _buffer(Z, n, f, w, dev)
+    ws, ws_bytes = _room(workspace, w, dev)
+    _check(lib().flashdp_activation_dp_grad(_buffer(dY, n, f, w, dev), z, int(bool(z_8bit)), B, T, d_out, int(dtype), activation_code(activation), C, sigma, seed, layer,
+                                            _buffer(dZ, n, f, w, dev), _buffer(out_grad, d_out, _torch.float32, w, dev), _buffer(out_norms, B, _torch.float32, w, dev),
                                             ws, ws_bytes, st, int(bool(accumulate)), int(bool(add_noise))), w)
 
 
 def flashdp_layernorm_forward(X, gamma, beta, rows: int, d: int, dtype: int, eps: float, Y, mean=None, rstd=None, stream=None):
     """Y = (X - mean) rstd gamma + beta over rows of d features; mean and rstd [rows] fp32 are kept for the backward pass if given."""
     w, f = "flashdp_layernorm_forward", _float_type(dtype)
-    st = _here(X, stream, w)
-    _check(lib().flashdp_layernorm_forward(_buffer(X, rows * d, f, w), _buffer(gamma, d, f, w), _buffer(beta, d, f, w), rows, d, int(dtype), eps,
-                                           _buffer(Y, rows * d, f, w), _buffer(mean, rows, _torch.float32, w), _buffer(rstd, rows, _torch.float32, w), st), w)
+    st, dev = _here(X, stream, w)
+    _check(lib().flashdp_layernorm_forward(_buffer(X, rows * d, f, w, dev), _buffer(gamma, d, f, w, dev), _buffer(beta, d, f, w, dev), rows, d, int(dtype), eps,
+                                           _buffer(Y, rows * d, f, w, dev), _buffer(mean, rows, _torch.float32, w, dev), _buffer(rstd, rows, _torch.float32, w, dev), st), w)
 
 
 def flashdp_layernorm_workspace_bytes(B: int, T: int, d: int, dtype: int, bias: bool = True) -> int:
@@ -399,11 +401,11 @@ def flashdp_layernorm_dp_grad(X, dY, gamma, mean, rstd, B: int, T: int, d: int, 
                               out_norms=None, bias: bool = True, workspace=None, stream=None, accumulate: bool = False, add_noise: bool = True):
     """dX and the clipped, noised gradient of gamma and beta (out_grad [2, d] fp32; [d] without a bias; or None)."""
     w, f, n = "flashdp_layernorm_dp_grad", _float_type(dtype), B * T * d
-    st = _here(X, stream, w)
-    ws, ws_bytes = _room(workspace)
-    _check(lib().flashdp_layernorm_dp_grad(_buffer(X, n, f, w), _buffer(dY, n, f, w), _buffer(gamma, d, f, w), _buffer(mean, B * T, _torch.float32, w),
-                                           _buffer(rstd, B * T, _torch.float32, w), B, T, d, int(dtype), C, sigma, seed, layer, _buffer(dX, n, f, w),
-                                           _buffer(out_grad, (2 if bias else 1) * d, _torch.float32, w), _buffer(out_norms, B, _torch.float32, w), int(bool(bias)),
+    st, dev = _here(X, stream, w)
+    ws, ws_bytes = _room(workspace, w, dev)
+    _check(lib().flashdp_layernorm_dp_grad(_buffer(X, n, f, w, dev), _buffer(dY, n, f, w, dev), _buffer(gamma, d, f, w, dev), _buffer(mean, B * T, _torch.float32, w, dev),
+                                           _buffer(rstd, B * T, _torch.float32, w, dev), B, T, d, int(dtype), C, sigma, seed, layer, _buffer(dX, n, f, w, dev),
+                                           _buffer(out_grad, (2 if bias else 1) * d, _torch.float32, w, dev), _buffer(out_norms, B, _torch.float32, w, dev), int(bool(bias)),
                                            ws, ws_bytes, st, int(bool(accumulate)), int(bool(add_noise))), w)
 
 
@@ -413,16 +415,16 @@ def flashdp_checkpoint8_bytes(rows: int, d: int) -> int:
 
 def flashdp_checkpoint8_pack(X, rows: int, d: int, dtype: int, packed, stream=None):
     w, f = "flashdp_checkpoint8_pack", _float_type(dtype)
-    st = _here(X, stream, w)
-    _check(lib().flashdp_checkpoint8_pack(_buffer(X, rows * d, f, w), rows, d, int(dtype),
-                                          _buffer(packed, flashdp_checkpoint8_bytes(rows, d), _torch.uint8, w), st), w)
+    st, dev = _here(X, stream, w)
+    _check(lib().flashdp_checkpoint8_pack(_buffer(X, rows * d, f, w, dev), rows, d, int(dtype),
+                                          _buffer(packed, flashdp_checkpoint8_bytes(rows, d), _torch.uint8, w, dev), st), w)
 
 
 def flashdp_checkpoint8_unpack(packed, rows: int, d: int, dtype: int, X, stream=None):
     w, f = "flashdp_checkpoint8_unpack", _float_type(dtype)
-    st = _here(packed, stream, w)
-    _check(lib().flashdp_checkpoint8_unpack(_buffer(packed, flashdp_checkpoint8_bytes(rows, d), _torch.uint8, w), rows, d, int(dtype),
-                                            _buffer(X, rows * d, f, w), st), w)
+    st, dev = _here(packed, stream, w)
+    _check(lib().flashdp_checkpoint8_unpack(_buffer(packed, flashdp_checkpoint8_bytes(rows, d), _torch.uint8, w, dev), rows, d, int(dtype),
+                                            _buffer(X, rows * d, f, w, dev), st), w)
 
 
 def flashdp_workspace_bytes_checkpoint8(layers, B: int, T: int, dtype: int, schedule=SCHEDULE_SCRATCH) -> int:
@@ -434,17 +436,17 @@ def flashdp_block_dp_grad_checkpoint8(layers, B: int, T: int, dtype: int, schedu
                                       accumulate: bool = False, add_noise: bool = True):
     """flashdp_block_dp_grad_micro with each layer's X an 8-bit checkpoint (a uint8 tensor of flashdp_checkpoint8_bytes(B * T, d_in))."""
     w, f = "flashdp_block_dp_grad_checkpoint8", _float_type(dtype)
-    arr, st = layers, None
+    arr, st, dev = layers, None, None
     if isinstance(layers, (list, tuple)):
         for L in layers:
-            st = _here(L["X"], stream, w)
-            _buffer(L["X"], flashdp_checkpoint8_bytes(B * T, L["d_in"]), _torch.uint8, w)
-            _buffer(L["dY"], B * T * L["d_out"], f, w)
-            _buffer(L["out_grad"], L["d_in"] * L["d_out"], _torch.float32, w)
-            _buffer(L.get("out_norms"), B, _torch.float32, w)
+            st, dev = _here(L["X"], stream, w)
+            _buffer(L["X"], flashdp_checkpoint8_bytes(B * T, L["d_in"]), _torch.uint8, w, dev)
+            _buffer(L["dY"], B * T * L["d_out"], f, w, dev)
+            _buffer(L["out_grad"], L["d_in"] * L["d_out"], _torch.float32, w, dev)
+            _buffer(L.get("out_norms"), B, _torch.float32, w, dev)
         arr = make_layers(layers)
     else:
-        st = _stream_handle(stream)
-    ws, ws_bytes = _room(workspace)
+        st, dev = _stream_handle(stream), _torch.cuda.current_device() if workspace is not None else None
+    ws, ws_bytes = _room(workspace, w, dev)
     _check(lib().flashdp_block_dp_grad_checkpoint8(arr, len(arr), B, T, int(dtype), schedule_code(schedule), ws, ws_bytes, st,
                                                    int(bool(accumulate)), int(bool(add_noise))), w)

@@ -9,8 +9,8 @@ namespace flashdp {
 namespace api {
 
 __attribute__((visibility("hidden"))) int current_device(int* dev);
-// At least `need` bytes of the library-owned workspace of the current device, grown if need be - but not while `stream` is
-// being captured, where FLASHDP_WORKSPACE_TOO_SMALL is the answer instead.
+// At least `need` bytes of the library-owned workspace of the current device, grown if need be; FLASHDP_WORKSPACE_TOO_SMALL while `stream` is
+// being captured.
 __attribute__((visibility("hidden"))) int library_workspace(size_t need, hipStream_t stream, void** ptr);
 __attribute__((visibility("hidden"))) int64_t compute_units();
 __attribute__((visibility("hidden"))) int forward_override();   // FLASHDP_FORWARD, or -1

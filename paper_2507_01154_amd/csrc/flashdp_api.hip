@@ -1124,9 +1124,12 @@ namespace api {
 
 int current_device(int* dev) { return device_or_error(dev); }
 int library_workspace(size_t need, hipStream_t stream, void** ptr) {
+  // (a graph would keep the address, and a later call that grows the workspace frees it)
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
+  if (capture != hipStreamCaptureStatusNone) return FLASHDP_WORKSPACE_TOO_SMALL;
   size_t got = 0;
-  const int st = owned_workspace(need, ptr, &got, 0, 0, stream);
-  return st != FLASHDP_OK ? st : got < need ? FLASHDP_WORKSPACE_TOO_SMALL : FLASHDP_OK;
+  return owned_workspace(need, ptr, &got);
 }
 int64_t compute_units() { return plan_cus(); }
 int forward_override() { return env().forward; }

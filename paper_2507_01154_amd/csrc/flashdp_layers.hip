@@ -28,6 +28,7 @@ namespace {
 constexpr int64_t GRID_LIMIT = (int64_t(1) << 31) - 1;
 constexpr int64_t FEATURE_LIMIT = int64_t(1) << 30;      // columns are computed in 32 bits
 constexpr int64_t ROW_LIMIT = int64_t(1) << 40;
+constexpr int64_t ELEMENT_LIMIT = int64_t(1) << 58;      // offsets and sizes in bytes are computed in 64 bits
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -37,11 +38,11 @@ inline bool valid_clip(float C, float sigma) { return C > 0.0f && std::isfinite(
 
 int check_rows(int64_t rows, int64_t d) {
   if (rows <= 0 || d <= 0) return FLASHDP_INVALID_ARGUMENT;
-  return rows >= ROW_LIMIT || d > FEATURE_LIMIT ? FLASHDP_UNSUPPORTED_SHAPE : FLASHDP_OK;
+  return rows >= ROW_LIMIT || d > FEATURE_LIMIT || rows > ELEMENT_LIMIT / d ? FLASHDP_UNSUPPORTED_SHAPE : FLASHDP_OK;
 }
 int check_samples(int64_t B, int64_t T, int64_t d) {
   if (B <= 0 || T <= 0 || d <= 0) return FLASHDP_INVALID_ARGUMENT;
-  return B >= (int64_t(1) << 20) || T >= (int64_t(1) << 31) || B * T >= ROW_LIMIT || d > FEATURE_LIMIT ? FLASHDP_UNSUPPORTED_SHAPE : FLASHDP_OK;
+  return B >= (int64_t(1) << 20) || T >= (int64_t(1) << 31) ? FLASHDP_UNSUPPORTED_SHAPE : check_rows(B * T, d);
 }
 
 // f(integral_constant<DT>) for the storage type of a call
@@ -516,6 +517,8 @@ static size_t unpacked_bytes(const flashdp_layer_t* layers, int n_layers, int64_
 
 size_t flashdp_workspace_bytes_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule) {
   const size_t need = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, schedule);
+  for (int l = 0; need != 0 && l < n_layers; ++l)
+    if (check_samples(B, T, layers[l].d_in) != FLASHDP_OK) return 0;
   return need == 0 ? 0 : unpacked_bytes(layers, n_layers, B, T, dtype) + need;
 }
 
@@ -532,6 +535,8 @@ int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layer
   if (B <= 0 || T <= 0) return FLASHDP_INVALID_ARGUMENT;
   for (int l = 0; l < n_layers; ++l)
     if (layers[l].d_in <= 0 || layers[l].d_out <= 0) return FLASHDP_INVALID_ARGUMENT;
+  for (int l = 0; l < n_layers; ++l)
+    if (check_samples(B, T, layers[l].d_in) != FLASHDP_OK) return FLASHDP_UNSUPPORTED_SHAPE;
   const size_t inner = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, schedule);
   if (inner == 0) return FLASHDP_UNSUPPORTED_SHAPE;
   const size_t room = unpacked_bytes(layers, n_layers, B, T, dtype);

@@ -710,3 +710,28 @@ def test_buffers_that_do_not_fit_are_refused():
         F.flashdp_layernorm_forward(x, w[0], None, 8, 16, F.BF16, 1e-5, y, n[:4], n)
     with pytest.raises(F.FlashDPError):      # a view that starts between two 16-byte boundaries
         call(x=torch.zeros(200, dtype=torch.bfloat16, device=DEV)[1:129].view(8, 16))
+
+
+def test_the_library_workspace_is_not_taken_by_a_graph():
+    """Large enough or not: a graph would keep its address past the call that grows it."""
+    dy, x, g = torch.randn(2, 40, 64, device=DEV), torch.randn(2, 40, 64, device=DEV), torch.zeros(64, device=DEV)
+    gam, mean, gn = torch.ones(64, device=DEV), torch.zeros(80, device=DEV), torch.zeros(2, 64, device=DEV)
+    packed = torch.zeros(F.flashdp_checkpoint8_bytes(80, 64), dtype=torch.uint8, device=DEV)
+    L = [dict(X=packed, dY=dy, d_in=64, d_out=64, C=1.0, sigma=0.0, seed=0, layer=0, out_grad=torch.zeros(64, 64, device=DEV), out_norms=None)]
+    calls = [lambda: F.flashdp_activation_dp_grad(dy, None, False, 2, 40, 64, F.F32, None, 1.0, 0.0, 0, 0, None, g),
+             lambda: F.flashdp_layernorm_dp_grad(x, dy, gam, mean, mean, 2, 40, 64, F.F32, 1.0, 0.0, 0, 0, None, gn),
+             lambda: F.flashdp_block_dp_grad_checkpoint8(L, 2, 40, F.F32, "twopass")]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in calls:
+            with pytest.raises(F.FlashDPError) as e:
+                call()
+            assert e.value.status == F.WORKSPACE_TOO_SMALL
+        g.add_(1.0)
+    del graph
+    for call in calls:
+        call()
+    torch.cuda.synchronize()

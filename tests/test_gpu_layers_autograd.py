@@ -180,3 +180,42 @@ def test_layers_without_an_epilogue_take_the_path_they_took():
     lin = DPLinear(64, 40, C=1.0, sigma=0.0, device=DEV)
     x = torch.randn(3, 20, 64, device=DEV).bfloat16()
     assert torch.equal(lin(x), torch.matmul(x, lin.weight.t()))
+
+
+@pytest.mark.parametrize("checkpoint", [None, "8bit"])
+def test_a_captured_step_gives_what_an_eager_one_gives(checkpoint):
+    """Forward and backward pass in a graph, replayed beside eager work that makes the library's workspace grow.  The captured modules are never
+    run eagerly."""
+    eager, captured = (modules(torch.bfloat16, 64, 96, checkpoint, sigma=0.5) for _ in range(2))
+    for a, b in zip(eager, captured):
+        a.keep_fp32_grad = b.keep_fp32_grad = False
+        a.load_state_dict(b.state_dict())
+    x, dy = torch.empty(3, 40, 64, device=DEV, dtype=torch.bfloat16), torch.empty(3, 40, 64, device=DEV, dtype=torch.bfloat16)
+
+    def step(ms):
+        ps = [p for m in ms for p in m.parameters() if p.requires_grad]
+        return torch.autograd.grad(block(*ms, x), ps, dy)
+
+    def draw(seed):
+        torch.manual_seed(seed)
+        x.normal_()
+        dy.normal_()
+
+    draw(1)
+    want = [t.clone() for t in step(eager)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(captured)
+    for rep in range(3):
+        draw(rep)
+        want = [t.clone() for t in step(eager)]
+        big = 256 << rep                     # a larger layer each time
+        o = torch.empty(big, big, device=DEV)
+        a = torch.ones(2, 64, big, device=DEV, dtype=torch.bfloat16)
+        F.flashdp_block_dp_grad([dict(X=a, dY=a, d_in=big, d_out=big, C=1.0, sigma=0.0, seed=0, layer=0, out_grad=o)], 2, 64, F.BF16, "scratch")
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g, w), rep

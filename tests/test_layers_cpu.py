@@ -168,3 +168,41 @@ def test_no_kernel_of_the_layers_spills_registers(tmp_path):
     assert len(kernels) > 40
     for k, u in kernels.items():
         assert u.get("VGPRs Spill", 0) == 0 and u.get("ScratchSize [bytes/lane]", 0) == 0, (k, u)
+
+
+def test_sizes_whose_bytes_pass_64_bits_are_refused():
+    rows, d = 1 << 39, 1 << 25                            # 2^64 elements
+    for name, good, change in (("flashdp_linear_forward", FORWARD, dict(rows=rows, d_in=d)), ("flashdp_linear_forward", FORWARD, dict(rows=rows, d_out=d)),
+                               ("flashdp_layernorm_forward", NORM, dict(rows=rows, d=d)), ("flashdp_activation_dp_grad", ACTIVATION, dict(B=1 << 9, T=1 << 30, d=d)),
+                               ("flashdp_layernorm_dp_grad", NORM_GRAD, dict(B=1 << 9, T=1 << 30, d=d)),
+                               ("flashdp_checkpoint8_pack", dict(a=A, rows=4, d=8, dtype=0, b=B_, stream=None), dict(rows=rows, d=d))):
+        refused(name, good, change, SHAPE)
+    assert F.flashdp_checkpoint8_bytes(rows, d) == 0 and F.flashdp_checkpoint8_bytes(1 << 33, 1 << 25) == (1 << 58) + (1 << 53)
+    assert F.flashdp_activation_workspace_bytes(1 << 9, 1 << 30, d, 0) == 0 and F.flashdp_layernorm_workspace_bytes(1 << 9, 1 << 30, d, 0) == 0
+
+
+def test_buffers_of_a_call_are_on_one_device():
+    from paper_2507_01154_amd import binding
+
+    class Elsewhere:      # a tensor as the checks see it, on device 1
+        dtype, shape, device = torch.float32, (8,), "cuda:1"
+        get_device, numel, is_contiguous, data_ptr, element_size = (lambda s: 1), (lambda s: 8), (lambda s: True), (lambda s: A), (lambda s: 4)
+
+    assert binding._buffer(Elsewhere(), 8, torch.float32, "x", 1) == A and binding._room(Elsewhere(), "x", 1) == (A, 32) and binding._room(None, "x", 0) == (None, 0)
+    for bad in (lambda: binding._buffer(Elsewhere(), 8, torch.float32, "x", 0), lambda: binding._room(Elsewhere(), "x", 0),
+                lambda: binding._room(torch.zeros(64), "x", 0), lambda: binding._buffer(Elsewhere(), 9, torch.float32, "x", 1)):
+        with pytest.raises(F.FlashDPError) as e:
+            bad()
+        assert e.value.status == INV
+
+
+def test_modules_refuse_inputs_of_other_shapes():
+    from paper_2507_01154_amd.autograd import DPLayerNorm, DPLinear
+    lin, ln = DPLinear(8, 8, device="cpu", bias=True, dtype=torch.float32), DPLayerNorm(8, device="cpu", dtype=torch.float32)
+    for shape in ((2, 4, 4), (2, 16), (8,), (64,)):       # 2 x 4 x 4: as many elements as four rows of 8
+        for m in (lin, ln):
+            with pytest.raises(TypeError):
+                m(torch.zeros(shape))
+    for residual in (torch.zeros(2, 1, 8), torch.zeros(2, 3, 8, dtype=torch.float64), torch.zeros(6, 8)):
+        with pytest.raises(TypeError):
+            lin(torch.zeros(2, 3, 8), residual=residual)
