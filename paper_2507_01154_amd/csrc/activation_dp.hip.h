@@ -22,6 +22,7 @@ struct ActivationArgs {
   const unsigned char* scales;    // of a checkpoint
   void* dZ;                       // may be null, may be dY
   float* partial;                 // [B][chunks][d]; may be null
+  double* squares;                // [B][col_tiles] sums of squares, where chunks == 1
   int64_t B, T, d;
   int chunks, rows_per_chunk;
   int col_tiles, log_ct;          // threads side by side: 1 << log_ct, chunks of 16 bytes each
@@ -32,6 +33,7 @@ template <int DT, int ACT, int ZK, bool TOKEN>
 __global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs a) {
   constexpr int N = Chunk<DT>::N, UNROLL = 4;
   __shared__ float part[TOKEN ? 1 : 256 * N];
+  __shared__ double square[4];
   const int ct = 1 << a.log_ct, rt = 256 >> a.log_ct;
   const int c = threadIdx.x & (ct - 1), r = threadIdx.x >> a.log_ct;
   const int64_t unit = blockIdx.x / a.col_tiles;                       // (sample, chunk of tokens), or rt samples
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs
   float sum[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) sum[k] = 0.0f;
-  if (left > 0) {
+  if (TOKEN || left > 0) {      // (TOKEN: threads beyond the row's end take part in its sum of squares, with zeros)
     const int64_t at = (row0 + r) * a.d + col, step = (int64_t)rt * a.d;          // elements; from row to row of this thread
     const char* dyp = (const char*)a.dY + at * Chunk<DT>::BYTES;
     const char* zp = (const char*)a.Z + at * (ZK == Z_EIGHT ? 1 : Chunk<DT>::BYTES);
@@ -67,7 +69,7 @@ __global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs
           if constexpr (ZK == Z_SAME) zr[u] = load_chunk<DT>(zp + u * step_z, 0, left);
           if constexpr (ZK == Z_EIGHT) {
             load_q<N>((const signed char*)zp + u * step_z, left, zq[u]);
-            sc[u] = sp[u * step_s];
+            sc[u] = !TOKEN || left > 0 ? sp[u * step_s] : 127;
           }
         }
       }
@@ -91,6 +93,11 @@ __global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs
                 store_chunk<DT_F32>(a.partial + at + u * step, 4 * q, left - 4 * q,
                                     u32x4_t{__builtin_bit_cast(uint32_t, f[4 * q]), __builtin_bit_cast(uint32_t, f[4 * q + 1]),
                                             __builtin_bit_cast(uint32_t, f[4 * q + 2]), __builtin_bit_cast(uint32_t, f[4 * q + 3])});
+              double q = 0.0;
+#pragma unroll
+              for (int k = 0; k < N; ++k) q += (double)f[k] * (double)f[k];
+              for (int off = ct >> 1; off > 0; off >>= 1) q += __shfl_xor(q, off, 64);
+              if (c == 0) a.squares[(row + (int64_t)u * rt) * a.col_tiles + (blockIdx.x - unit * a.col_tiles)] = q;
             }
           }
         }
@@ -109,13 +116,20 @@ __global__ __launch_bounds__(256) void activation_dp_kernel(const ActivationArgs
     // element e of the column tile: its N ct sums lie at [e % N][.. e / N ..]; one thread per element, neighbours side by side
     float* to = a.partial + unit * a.d;
     const int64_t first = (int64_t)(blockIdx.x - unit * a.col_tiles) * ct * N;
+    double q = 0.0;
     for (int e = threadIdx.x; e < ct * N; e += 256) {
       if (first + e >= a.d) break;
       const float* p = part + (e % N) * 256 + e / N;
       float s = 0.0f;
       for (int k = 0; k < rt; ++k) s += p[k * ct];
       to[first + e] = s;
+      q += (double)s * (double)s;
     }
+    if (a.chunks > 1) return;
+    q = wave_sum(q);
+    if ((threadIdx.x & 63) == 0) square[threadIdx.x >> 6] = q;
+    __syncthreads();
+    if (threadIdx.x == 0) a.squares[blockIdx.x] = (square[0] + square[1]) + (square[2] + square[3]);
   }
 }
 

@@ -65,9 +65,10 @@ hipError_t launch(void (*kernel)(Formal...), int64_t grid, int threads, size_t l
 
 struct VectorWs { size_t partial, g, squares, factors, total; int blocks; };
 
-VectorWs vector_ws(int64_t B, int64_t chunks, int64_t n) {
+// blocks: sums of squares per sample that the kernel before leaves, 0 if vector_sum_kernel does
+VectorWs vector_ws(int64_t B, int64_t chunks, int64_t n, int64_t blocks) {
   VectorWs w;
-  w.blocks = (int)((n + 63) / 64);
+  w.blocks = (int)(blocks ? blocks : (n + 63) / 64);
   w.partial = 0;
   w.g = align_up((size_t)B * chunks * n * 4, 256);
   w.squares = w.g + (chunks > 1 ? align_up((size_t)B * n * 4, 256) : 0);
@@ -76,14 +77,14 @@ VectorWs vector_ws(int64_t B, int64_t chunks, int64_t n) {
   return w;
 }
 
-// What comes after the partial sums: their sum, norms, clip factors, the clipped sum and its noise.
-hipError_t run_vector(VectorArgs& v, char* ws, const VectorWs& w, hipStream_t st) {
+// What comes after the partial sums: their sum (if summed is false), norms, clip factors, the clipped sum and its noise.
+hipError_t run_vector(VectorArgs& v, char* ws, const VectorWs& w, bool summed, hipStream_t st) {
   v.partial = reinterpret_cast<const float*>(ws + w.partial);
   v.g = reinterpret_cast<float*>(ws + (v.chunks > 1 ? w.g : w.partial));
   v.squares = reinterpret_cast<double*>(ws + w.squares);
   v.factors = reinterpret_cast<float*>(ws + w.factors);
   v.blocks = w.blocks;
-  hipError_t e = launch(vector_sum_kernel, v.B * v.blocks, 256, 0, st, v);
+  hipError_t e = summed ? hipSuccess : launch(vector_sum_kernel, v.B * v.blocks, 256, 0, st, v);
   if (e != hipSuccess) return e;
   const bool fold = v.B <= VECTOR_FOLD_B && v.B * v.blocks <= VECTOR_FOLD_SQUARES;
   if (!fold && (e = launch(vector_factors_kernel, (v.B + 3) / 4, 256, 0, st, v)) != hipSuccess) return e;
@@ -99,7 +100,12 @@ int64_t chunks_of(int64_t B, int64_t T, int64_t column_groups) {
   return std::max<int64_t>(1, std::min(want, (T + 15) / 16));
 }
 
-struct ActivationPlan { int log_ct; int64_t col_tiles, chunks, rows_per_chunk; bool token; };
+struct ActivationPlan {
+  int log_ct;
+  int64_t col_tiles, chunks, rows_per_chunk;
+  bool token;
+  int64_t squares() const { return chunks == 1 ? col_tiles : 0; }      // per sample, from the kernel
+};
 
 ActivationPlan activation_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   ActivationPlan p;
@@ -174,7 +180,7 @@ NormGradKernel norm_grad_kernel_of(int64_t d, int dtype, bool token) {
   return by_dtype(dtype, [&](auto dt) { return norm_grad_kernel<decltype(dt)::value>(columns, d % n == 0, token); });
 }
 
-struct NormPlan { int64_t columns, col_tiles, chunks, rows_per_chunk; bool token; };
+struct NormPlan { int64_t columns, col_tiles, chunks, rows_per_chunk, squares; bool token; };   // squares: per sample, from the kernel
 
 NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   NormPlan p;
@@ -189,6 +195,7 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   const int64_t k = p.token ? 1 : std::max<int64_t>(1, std::min(want, (T + fewest - 1) / fewest));
   p.rows_per_chunk = (T + k - 1) / k;
   p.chunks = (T + p.rows_per_chunk - 1) / p.rows_per_chunk;
+  p.squares = !held || p.chunks > 1 ? 0 : kernel.threads / (p.token ? kernel.rows : 1) / 64;
   return p;
 }
 
@@ -344,7 +351,8 @@ int flashdp_linear_forward(const void* X, const void* W, const void* bias, const
 
 size_t flashdp_activation_workspace_bytes(int64_t B, int64_t T, int64_t d_out, int dtype) {
   if (!valid_dtype(dtype) || check_samples(B, T, d_out) != FLASHDP_OK) return 0;
-  return vector_ws(B, activation_plan(B, T, d_out, dtype).chunks, d_out).total;
+  const ActivationPlan p = activation_plan(B, T, d_out, dtype);
+  return vector_ws(B, p.chunks, d_out, p.squares()).total;
 }
 
 int flashdp_activation_dp_grad(const void* dY, const void* Z, int z_8bit, int64_t B, int64_t T, int64_t d_out, int dtype, int activation,
@@ -360,7 +368,7 @@ int flashdp_activation_dp_grad(const void* dY, const void* Z, int z_8bit, int64_
     return FLASHDP_MISALIGNED;
   const ActivationPlan p = activation_plan(B, T, d_out, dtype);
   const int64_t rt = 256 >> p.log_ct, units = p.token ? (B + rt - 1) / rt : B * p.chunks;
-  const VectorWs w = vector_ws(B, p.chunks, d_out);
+  const VectorWs w = vector_ws(B, p.chunks, d_out, p.squares());
   if (units * p.col_tiles > GRID_LIMIT || B * w.blocks > GRID_LIMIT) return FLASHDP_UNSUPPORTED_SHAPE;
   if (out_grad && workspace && workspace_bytes < w.total) return FLASHDP_WORKSPACE_TOO_SMALL;
   int dev = 0;
@@ -372,6 +380,7 @@ int flashdp_activation_dp_grad(const void* dY, const void* Z, int z_8bit, int64_
   a.dY = dY; a.Z = Z; a.dZ = dZ;
   a.scales = use_z && z_8bit ? static_cast<const unsigned char*>(Z) + checkpoint8_scales_at(B * T, d_out) : nullptr;
   a.partial = out_grad ? reinterpret_cast<float*>(ws + w.partial) : nullptr;
+  a.squares = out_grad ? reinterpret_cast<double*>(ws + w.squares) : nullptr;
   a.B = B; a.T = T; a.d = d_out;
   a.chunks = (int)p.chunks; a.rows_per_chunk = (int)p.rows_per_chunk; a.col_tiles = (int)p.col_tiles; a.log_ct = p.log_ct;
   HIP_TRY(by_dtype(dtype, [&](auto dt) {
@@ -386,7 +395,7 @@ int flashdp_activation_dp_grad(const void* dY, const void* Z, int z_8bit, int64_
   v.n = d_out; v.B = B; v.chunks = a.chunks;
   v.C = C; v.noise_scale = add_noise ? sigma * C : 0.0f; v.seed = seed; v.layer = layer; v.field = FLASHDP_FIELD_BIAS;
   v.out = out_grad; v.out_norms = out_norms; v.accumulate = accumulate ? 1 : 0;
-  HIP_TRY(run_vector(v, ws, w, hs));
+  HIP_TRY(run_vector(v, ws, w, p.squares() != 0, hs));
   return FLASHDP_OK;
 }
 
@@ -414,7 +423,8 @@ int flashdp_layernorm_forward(const void* X, const void* gamma, const void* beta
 
 size_t flashdp_layernorm_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype, int bias) {
   if (!valid_dtype(dtype) || check_samples(B, T, d) != FLASHDP_OK) return 0;
-  return vector_ws(B, norm_plan(B, T, d, dtype).chunks, bias ? 2 * d : d).total;
+  const NormPlan p = norm_plan(B, T, d, dtype);
+  return vector_ws(B, p.chunks, bias ? 2 * d : d, p.squares).total;
 }
 
 int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, const float* mean, const float* rstd, int64_t B, int64_t T, int64_t d,
@@ -429,7 +439,7 @@ int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, 
     return FLASHDP_MISALIGNED;
   const int64_t n = bias ? 2 * d : d;
   const NormPlan p = norm_plan(B, T, d, dtype);
-  const VectorWs w = vector_ws(B, p.chunks, n);
+  const VectorWs w = vector_ws(B, p.chunks, n, p.squares);
   if (B * p.chunks * p.col_tiles > GRID_LIMIT || B * w.blocks > GRID_LIMIT || (p.columns > NORM_LONG && B * T > GRID_LIMIT)) return FLASHDP_UNSUPPORTED_SHAPE;
   if (out_grad && workspace && workspace_bytes < w.total) return FLASHDP_WORKSPACE_TOO_SMALL;
   int dev = 0;
@@ -440,6 +450,7 @@ int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, 
   NormGradArgs a;
   a.X = X; a.dY = dY; a.gamma = gamma; a.mean = mean; a.rstd = rstd; a.dX = dX;
   a.partial = out_grad ? reinterpret_cast<float*>(ws + w.partial) : nullptr;
+  a.squares = out_grad ? reinterpret_cast<double*>(ws + w.squares) : nullptr;
   a.B = B; a.T = T; a.d = d; a.chunks = (int)p.chunks; a.rows_per_chunk = (int)p.rows_per_chunk; a.bias = bias ? 1 : 0;
   if (p.columns <= NORM_LONG) {
     const NormGradKernel k = norm_grad_kernel_of(d, dtype, p.token);
@@ -457,7 +468,7 @@ int flashdp_layernorm_dp_grad(const void* X, const void* dY, const void* gamma, 
   v.n = n; v.B = B; v.chunks = a.chunks;
   v.C = C; v.noise_scale = add_noise ? sigma * C : 0.0f; v.seed = seed; v.layer = layer; v.field = FLASHDP_FIELD_NORM;
   v.out = out_grad; v.out_norms = out_norms; v.accumulate = accumulate ? 1 : 0;
-  HIP_TRY(run_vector(v, ws, w, hs));
+  HIP_TRY(run_vector(v, ws, w, p.squares != 0, hs));
   return FLASHDP_OK;
 }
 

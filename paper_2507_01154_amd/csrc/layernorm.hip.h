@@ -35,6 +35,7 @@ struct NormGradArgs {
   const float* rstd;
   void* dX;               // may be null, may be dY
   float* partial;         // [B][chunks][2 d] (d without a bias); may be null
+  double* squares;        // of the held rows' kernel, where chunks == 1: [B][waves of a sample] sums of squares
   int64_t B, T, d;
   int chunks, rows_per_chunk;
   int bias;
@@ -250,8 +251,11 @@ __global__ __launch_bounds__(THREADS) void layernorm_grad_kernel(const NormGradA
   if constexpr (TOKEN || ROWS == 1) {
     if (TOKEN && first + g >= last) return;
     float* to = a.partial + (TOKEN ? first + g : (int64_t)blockIdx.x) * a.d * (a.bias ? 2 : 1);
+    double square = 0.0;      // (columns that do not exist have sums of zero)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) square += (double)sg[c][k] * (double)sg[c][k] + (a.bias ? (double)sb[c][k] * (double)sb[c][k] : 0.0);
       const int64_t col = (int64_t)(c * NT + t) * N, left = a.d - col;
 #pragma unroll
       for (int q = 0; q < N; q += 4) {
@@ -259,9 +263,14 @@ __global__ __launch_bounds__(THREADS) void layernorm_grad_kernel(const NormGradA
         if (a.bias) store_sums4<EVEN>(to + a.d, col + q, left - q, sb[c] + q);
       }
     }
+    if (TOKEN || a.chunks == 1) {
+      square = wave_sum(square);
+      if ((t & 63) == 0) a.squares[(TOKEN ? first + g : (int64_t)blockIdx.x) * (NT / 64) + t / 64] = square;
+    }
   } else {
     // the rows of threads join their sums, NT * N columns of one of the two vectors at a time
     float* to = a.partial + (int64_t)blockIdx.x * a.d * (a.bias ? 2 : 1);
+    double square = 0.0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
 #pragma unroll
@@ -278,8 +287,13 @@ __global__ __launch_bounds__(THREADS) void layernorm_grad_kernel(const NormGradA
 #pragma unroll
           for (int q = 0; q < ROWS; ++q) s += lds[(e % N) * PITCH + q * NT + e / N];
           to[part * a.d + col] = s;
+          square += (double)s * (double)s;
         }
       }
+    }
+    if (a.chunks == 1) {
+      square = wave_sum(square);
+      if ((threadIdx.x & 63) == 0) a.squares[(int64_t)blockIdx.x * (THREADS / 64) + threadIdx.x / 64] = square;
     }
   }
 }

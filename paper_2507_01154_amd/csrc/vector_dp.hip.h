@@ -18,10 +18,10 @@ namespace flashdp {
 struct VectorArgs {
   const float* partial;   // [B][chunks][n]
   float* g;               // [B][n]; partial itself where chunks == 1
-  double* squares;        // [B][blocks] sums of squares of 64 elements each
+  double* squares;        // [B][blocks] sums of squares: of 64 elements each, or from the kernel before where chunks == 1
   float* factors;         // [B] clip factors, where they come from a launch of their own
   int64_t n, B;
-  int chunks, blocks;     // blocks = ceil(n / 64)
+  int chunks, blocks;
   float C, noise_scale;
   uint64_t seed;
   uint32_t layer, field;
@@ -30,7 +30,7 @@ struct VectorArgs {
   int accumulate;
 };
 
-// One workgroup per 64 elements of one sample's vector, its four waves taking every fourth chunk.
+// One workgroup per 64 elements of one sample's vector (blocks = ceil(n / 64)), its four waves taking every fourth chunk.
 __global__ __launch_bounds__(256) void vector_sum_kernel(const VectorArgs a) {
   __shared__ float part[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
