@@ -15,7 +15,10 @@ namespace flashdp {
 
 enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4 };
 
-__device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+// 1 / (1 + 2^u): s(v) for u = -v log2(e), a factor that folds into what v is made of
+__device__ __forceinline__ float logistic_of_exp2(float u) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u)); }
+constexpr float LOG2_E = 1.44269504f;
+constexpr float GELU_1 = 1.59576912f, GELU_3 = 1.59576912f * 0.044715f;      // 2 u = GELU_1 z + GELU_3 z^3
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
@@ -23,8 +26,8 @@ __device__ __forceinline__ float act_value(float z) {
   if constexpr (ACT == ACT_RELU) return z <= 0.0f ? 0.0f : z;     // (a comparison with NaN is false)
   const float c = fmaxf(z, -128.0f);
   if constexpr (ACT == ACT_GELU) return 0.5f * c * erfcf(-0.70710678f * z);
-  if constexpr (ACT == ACT_GELU_TANH) return c * logistic(1.5957691f * z * fmaf(0.044715f * z, z, 1.0f));
-  if constexpr (ACT == ACT_SILU) return c * logistic(z);
+  if constexpr (ACT == ACT_GELU_TANH) return c * logistic_of_exp2(z * fmaf(z * z, -LOG2_E * GELU_3, -LOG2_E * GELU_1));
+  if constexpr (ACT == ACT_SILU) return c * logistic_of_exp2(-LOG2_E * z);
 }
 
 template <int ACT>
@@ -34,11 +37,11 @@ __device__ __forceinline__ float act_slope(float z) {
   const float c = __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f);
   if constexpr (ACT == ACT_GELU) return fmaf(0.39894228f * c, __expf(-0.5f * c * c), 0.5f * erfcf(-0.70710678f * z));
   if constexpr (ACT == ACT_GELU_TANH) {
-    const float cc = c * c, s = logistic(1.5957691f * z * fmaf(0.044715f * c, c, 1.0f));
-    return fmaf(c * 1.5957691f * fmaf(3.0f * 0.044715f, cc, 1.0f) * (1.0f - s), s, s);   // s + z s (1 - s) d(2 u)/dz
+    const float cc = c * c, s = logistic_of_exp2(z * fmaf(cc, -LOG2_E * GELU_3, -LOG2_E * GELU_1));
+    return fmaf(c * fmaf(cc, 3.0f * GELU_3, GELU_1) * (1.0f - s), s, s);   // s + z s (1 - s) d(2 u)/dz
   }
   if constexpr (ACT == ACT_SILU) {
-    const float s = logistic(z);
+    const float s = logistic_of_exp2(-LOG2_E * z);
     return fmaf(c * (1.0f - s), s, s);
   }
 }
