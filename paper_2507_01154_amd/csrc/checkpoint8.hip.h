@@ -71,21 +71,26 @@ __device__ __forceinline__ uint32_t checkpoint8_quantise4(const float* f, float 
   return hi << 16 | lo;
 }
 
-// The values of N q, a byte each: a byte with its sign bit turned is q + 128, which converts in one instruction.  A zero among those bytes is q = -128, a value that was not finite; words that have one are gone through again.
+// The values of N q, a byte each, of a block of the given scale 2^e: a byte with its sign bit turned is u = q + 128, which converts in one
+// instruction, and u 2^e - 128 2^e is exact.  Gone through again are words with a zero among those bytes, which is q = -128, a value that was
+// not finite, and blocks of e = 121, where 128 2^e overflows.
 template <int N>
 __device__ __forceinline__ void checkpoint8_values(const uint32_t (&v)[N / 4], float scale, float (&f)[N]) {
+  const float offset = -128.0f * scale;
   uint32_t zero = 0;
 #pragma unroll
   for (int k = 0; k < N / 4; ++k) {
     const uint32_t u = v[k] ^ 0x80808080u;
     zero |= (u - 0x01010101u) & ~u & 0x80808080u;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) f[4 * k + b] = ((float)((u >> (8 * b)) & 0xFFu) - 128.0f) * scale;
+    for (int b = 0; b < 4; ++b) f[4 * k + b] = fmaf((float)((u >> (8 * b)) & 0xFFu), scale, offset);
   }
-  if (zero) {
+  if (zero || !finite_f32(offset)) {
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (((v[k >> 2] >> (8 * (k & 3))) & 0xFFu) == 0x80u) f[k] = __builtin_bit_cast(float, 0x7FC00000u);
+    for (int k = 0; k < N; ++k) {
+      const uint32_t byte = (v[k >> 2] >> (8 * (k & 3))) & 0xFFu;
+      f[k] = byte == 0x80u ? __builtin_bit_cast(float, 0x7FC00000u) : (float)(signed char)byte * scale;
+    }
   }
 }
 
