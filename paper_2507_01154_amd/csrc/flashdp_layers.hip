@@ -93,13 +93,6 @@ hipError_t run_vector(VectorArgs& v, char* ws, const VectorWs& w, bool summed, h
   return launch(fold ? vector_clip_kernel<true, 16> : vector_clip_kernel<false, 16>, (v.n + 15) / 16, 256, 0, st, v);
 }
 
-// Tokens per partial sum: about four workgroups per compute unit (column_groups of them per chunk of tokens), and no fewer than
-// 16 tokens, below which writing and reading the partial sums shows.
-int64_t chunks_of(int64_t B, int64_t T, int64_t column_groups) {
-  const int64_t want = (4 * 256 + B * column_groups - 1) / (B * column_groups);
-  return std::max<int64_t>(1, std::min(want, (T + 15) / 16));
-}
-
 struct ActivationPlan {
   int log_ct;
   int64_t col_tiles, chunks, rows_per_chunk;
@@ -114,8 +107,11 @@ ActivationPlan activation_plan(int64_t B, int64_t T, int64_t d, int dtype) {
   while (p.log_ct < 6 && (int64_t(1) << p.log_ct) < columns) ++p.log_ct;
   p.col_tiles = (columns + (1 << p.log_ct) - 1) >> p.log_ct;
   p.token = T == 1;
-  const int64_t k = p.token ? 1 : chunks_of(B, T, p.col_tiles);
-  p.rows_per_chunk = (T + k - 1) / k;
+  // tokens per partial sum: at most the six workgroups per compute unit that are there at a time (8192 x 3072, 8 samples, Z in 8 bits, all three
+  // kernels: two 38.2, four 36.4, six 34.7, eight 37.5 us), and whole trips of the kernel's loop, 16 tokens or more, below which writing
+  // and reading the partial sums shows
+  const int64_t k = p.token ? 1 : std::max<int64_t>(1, 6 * 256 / (B * p.col_tiles)), trip = 4 * (256 >> p.log_ct);
+  p.rows_per_chunk = std::min(T, ((T + k - 1) / k + trip - 1) / trip * trip);
   p.chunks = (T + p.rows_per_chunk - 1) / p.rows_per_chunk;
   return p;
 }
