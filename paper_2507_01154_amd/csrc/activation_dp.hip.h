@@ -4,6 +4,8 @@
 // Memory bound: dY and Z in, dZ out, 6 bytes an element in 16-bit types and 5 with Z in 8 bits.  A thread owns one chunk of 16 bytes of
 // a row and goes down the tokens of its workgroup's chunk, so the sums over tokens stay in registers; the rows of
 // threads join theirs in LDS at the end.  Four rows' loads are in flight per thread.
+//
+// 8192 x 3072 bf16, GELU (tanh form), Z in 8 bits, 8 samples: 25 us = 5.0 TB/s, the vector instructions close behind the bytes.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -11,7 +11,7 @@
 // of which every fp16 number is a multiple.  An element that is not finite is kept as q = -128 and comes back as NaN.
 // Layout: q of all rows, [rows][d] int8, up to a multiple of 16 bytes; then e + 127 of all blocks, [rows][ceil(d / 32)] uint8.
 //
-// Memory bound: 2 (4) + 33/32 bytes an element.  Four lanes (fp32: eight) hold a block and agree on m by exchanges inside the wave.
+// Memory bound: 2 (4) + 33/32 bytes an element; 16384 x 5120 bf16 packed in 52 us = 4.9 TB/s, unpacked in 38 (a part from the caches).  Four lanes (fp32: eight) hold a block and agree on m by exchanges inside the wave.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

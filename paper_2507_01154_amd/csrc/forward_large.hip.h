@@ -10,6 +10,10 @@
 // soon as its last quadrant is issued - lo x first, lo x second, hi x second, hi x first, the halves of W changing roles from step to step -
 // with the reads of a quadrant issued one to two quadrants ahead.  The order is held by scheduling barriers; the waits for LDS are the
 // compiler's, those for the direct loads, which it does not see, are written by hand.
+//
+// Bound by the matrix cores at the clock they hold: bf16 8192 x 5120 -> 13824 with SiLU and Z 948 us = 1.22 PFLOP/s on 256 x 256.  Short
+// rows by the epilogues, which workgroups that started together reach together: 8192 x 768 -> 3072 on 128 x 128 51 us, with GELU and Z
+// in 8 bits 62 (every second workgroup started 4 us late: 1.6 us more).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

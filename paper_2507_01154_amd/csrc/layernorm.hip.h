@@ -8,6 +8,9 @@
 // in a stream with an offset.  Backward, a thread holds the same columns of every row it meets, so the sums over tokens of dgamma and
 // dbeta stay in registers too: one workgroup goes through a chunk of a sample's tokens and leaves one partial sum
 // (vector_dp.hip.h adds them up).  Rows that no register file holds are read again for every sum.
+//
+// 16384 x 5120 bf16: forward 64 us = 5.2 TB/s; backward 113 us = 4.5 TB/s with 16 waves a compute unit, which is what 111 registers leave.  8168 x 768
+// fp16, 8 samples: 7.8 and 12.4 us, two rounds of rows a workgroup (the next round's loads ahead of a row's sums: 2 us more).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

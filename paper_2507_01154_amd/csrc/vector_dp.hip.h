@@ -4,7 +4,9 @@
 //
 // The kernels that go over the tokens leave one partial sum per chunk of tokens; their order is fixed, nothing is added
 // atomically, so results repeat to the bit.  Squares are added up in fp64 (an element of 1e20 does not overflow its norm).
-// Bound by launches and latency: B (chunks + 1) n floats, a few MB at most next to the activations that were read before.
+// Bound by launches and latency: B (chunks + 1) n floats, a few MB at most next to the activations that were read before.  8 samples of 3072
+// in 32 chunks: 4.7 us for the sums, 4.6 for the rest, some 2 of each the launch; where the kernel before has all of a sample's
+// tokens in one workgroup it leaves the squares as well and the first of the two falls away (256 samples of 512: 11.0 us in all, 9.5 so).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
