@@ -5,7 +5,7 @@
 // The kernels that go over the tokens leave one partial sum per chunk of tokens; their order is fixed, nothing is added
 // atomically, so results repeat to the bit.  Squares are added up in fp64 (an element of 1e20 does not overflow its norm).
 // Bound by launches and latency: B (chunks + 1) n floats, a few MB at most next to the activations that were read before.  8 samples of 3072
-// in 32 chunks: 4.7 us for the sums, 4.6 for the rest, some 2 of each the launch; where the kernel before has all of a sample's
+// in 32 chunks: 4.6 us for the sums, 4.4 for the rest, some 2 of each the launch; where the kernel before has all of a sample's
 // tokens in one workgroup it leaves the squares as well and the first of the two falls away (256 samples of 512: 11.0 us in all, 9.5 so).
 #pragma once
 #include <hip/hip_runtime.h>
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void vector_sum_kernel(const VectorArgs a) {
   float s = 0.0f;
   if (col < a.n) {
     const float* p = a.partial + i * a.chunks * a.n + col;
-#pragma unroll 4
+#pragma unroll 8
     for (int k = wave; k < a.chunks; k += 4) s += p[(int64_t)k * a.n];
   }
   part[wave][lane] = s;
@@ -82,9 +82,23 @@ constexpr int VECTOR_FOLD_B = 1024;             // factors kept in LDS
 constexpr int64_t VECTOR_FOLD_SQUARES = 8192;   // B * blocks doubles that every workgroup reads: 64 KB from the caches
 template <bool FOLD, int COLS>
 __global__ __launch_bounds__(256) void vector_clip_kernel(const VectorArgs a) {
-  constexpr int ROWS = 256 / COLS;
+  constexpr int ROWS = 256 / COLS, EARLY = 4;
   __shared__ float fac[FOLD ? VECTOR_FOLD_B : 1];
   __shared__ float part[ROWS][COLS];
+  const int c = threadIdx.x % COLS, r = threadIdx.x / COLS;
+  const int64_t col = (int64_t)blockIdx.x * COLS + c;
+  // what does not depend on the factors goes first: the first samples' elements, the old output, the noise
+  float early[EARLY], old = 0.0f, noise = 0.0f;
+#pragma unroll
+  for (int k = 0; k < EARLY; ++k) early[k] = col < a.n && r + k * ROWS < a.B ? a.g[(int64_t)(r + k * ROWS) * a.n + col] : 0.0f;
+  if (r == 0 && col < a.n) {
+    if (a.accumulate) old = a.out[col];
+    if (a.noise_scale != 0.0f) {
+      const Normals4 z = noise_group(a.seed, a.layer, (uint64_t)(col >> 2), a.field);
+      const int e = (int)(col & 3);
+      noise = e == 0 ? z.z[0] : e == 1 ? z.z[1] : e == 2 ? z.z[2] : z.z[3];
+    }
+  }
   if constexpr (FOLD) {
     int lanes = 64;
     while (lanes > 1 && lanes * a.B > 256) lanes >>= 1;
@@ -99,12 +113,13 @@ __global__ __launch_bounds__(256) void vector_clip_kernel(const VectorArgs a) {
     }
     __syncthreads();
   }
-  const int c = threadIdx.x % COLS, r = threadIdx.x / COLS;
-  const int64_t col = (int64_t)blockIdx.x * COLS + c;
   float s = 0.0f;
   if (col < a.n) {
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k)
+      if (r + k * ROWS < a.B) s = fmaf(FOLD ? fac[r + k * ROWS] : a.factors[r + k * ROWS], early[k], s);
 #pragma unroll 8
-    for (int64_t i = r; i < a.B; i += ROWS) s = fmaf(FOLD ? fac[i] : a.factors[i], a.g[i * a.n + col], s);
+    for (int64_t i = r + EARLY * ROWS; i < a.B; i += ROWS) s = fmaf(FOLD ? fac[i] : a.factors[i], a.g[i * a.n + col], s);
   }
   part[r][c] = s;
   __syncthreads();
@@ -112,12 +127,8 @@ __global__ __launch_bounds__(256) void vector_clip_kernel(const VectorArgs a) {
   s = 0.0f;
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) s += part[k][c];
-  if (a.accumulate) s += a.out[col];
-  if (a.noise_scale != 0.0f) {
-    const Normals4 z = noise_group(a.seed, a.layer, (uint64_t)(col >> 2), a.field);
-    const int e = (int)(col & 3);
-    s = fmaf(a.noise_scale, e == 0 ? z.z[0] : e == 1 ? z.z[1] : e == 2 ? z.z[2] : z.z[3], s);
-  }
+  if (a.accumulate) s += old;
+  if (a.noise_scale != 0.0f) s = fmaf(a.noise_scale, noise, s);
   a.out[col] = s;
 }
 
