@@ -735,3 +735,83 @@ def test_the_library_workspace_is_not_taken_by_a_graph():
     for call in calls:
         call()
     torch.cuda.synchronize()
+
+
+# ---- offsets that pass 32 bits ----------------------------------------------------------------------
+
+LONG = (1100000, 2048)      # rows and features: 2.25e9 elements, 4.5 GB in 16 bits
+LOOK = [0, 1, 524287, 524288, 1048575, 1048576, 1099990, 1099999]      # rows on both sides of 2^30 and 2^31 elements, and the last
+
+
+def long_rows(d=LONG[1], rows=LONG[0]):
+    return torch.empty(rows, d, dtype=torch.bfloat16, device=DEV).normal_()
+
+
+@pytest.mark.parametrize("K,D", [(2048, 40), (40, 2048), (2047, 24), (24, 2047)])
+def test_forward_of_long_inputs(K, D):
+    """Tolerance: one rounding to bfloat16 and fp32 sums of at most 2048 products."""
+    rows = LONG[0]
+    x, w, y = long_rows(K), torch.randn(D, K, device=DEV).bfloat16(), torch.empty(rows, D, dtype=torch.bfloat16, device=DEV)
+    F.flashdp_linear_forward(x, w, None, None, rows, K, D, F.BF16, None, y)
+    torch.cuda.synchronize()
+    x64, w64 = x[LOOK].cpu().double(), w.cpu().double()
+    want, size = x64 @ w64.T, x64.abs() @ w64.abs().T
+    assert bool(((y[LOOK].cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + K * 2.0 ** -24 * size).all())
+
+
+def test_normalisation_of_long_inputs():
+    """Forward and dX on the rows looked at: fp32 sums of 2048 terms and one rounding; the parameters' gradients against sums in 64 bits over all rows.  Those are
+    fp32 sums of 2^12 terms at most in a row, so off by less than 2^-12 of the sum of magnitudes; a row read elsewhere moves them by more."""
+    B, (rows, d) = 2, LONG
+    T = rows // B
+    x, dy = long_rows(), long_rows()
+    gam, bet = torch.randn(d, device=DEV).bfloat16(), torch.randn(d, device=DEV).bfloat16()
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, g, n = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty(2, d, device=DEV), torch.empty(B, device=DEV)
+    F.flashdp_layernorm_forward(x, gam, bet, rows, d, F.BF16, 1e-5, y, mean, rstd)
+    F.flashdp_layernorm_dp_grad(x, dy, gam, mean, rstd, B, T, d, F.BF16, 1e6, 0.0, 0, 0, dx, g, n)
+    torch.cuda.synchronize()
+    x64, dy64, g64, b64 = x[LOOK].cpu().double(), dy[LOOK].cpu().double(), gam.cpu().double(), bet.cpu().double()
+    mu = x64.mean(1, keepdim=True)
+    r = ((x64 - mu).square().mean(1, keepdim=True) + 1e-5) ** -0.5
+    xh, a = (x64 - mu) * r, dy64 * g64
+    dx64 = r * (a - a.mean(1, keepdim=True) - xh * (a * xh).mean(1, keepdim=True))
+    for got, want in ((y[LOOK], xh * g64 + b64), (dx[LOOK], dx64)):
+        assert bool(((got.cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-3 * 2.0 ** -8 * want.abs().max()).all())
+    del y, dx
+    total, size, norms = torch.zeros(2, d, device=DEV, dtype=torch.float64), torch.zeros(2, d, device=DEV, dtype=torch.float64), []
+    for i in range(B):
+        s = torch.zeros(2, d, device=DEV, dtype=torch.float64)
+        for k in range(i * T, (i + 1) * T, 50000):
+            e = min(k + 50000, (i + 1) * T)
+            dyk = dy[k:e].double()
+            p = dyk * ((x[k:e].double() - mean[k:e, None].double()) * rstd[k:e, None].double())
+            s += torch.stack((p.sum(0), dyk.sum(0)))
+            size += torch.stack((p.abs().sum(0), dyk.abs().sum(0)))
+        total += s
+        norms.append(float(s.norm()))
+    assert bool(((g.double() - total).abs() <= 2.0 ** -12 * size).all())
+    for got, want in zip(n.tolist(), norms):
+        assert abs(got - want) <= 1e-3 * want
+
+
+def test_activation_gradient_and_checkpoints_of_long_inputs():
+    """dZ from a checkpoint of Z (ReLU: exact), the bias's gradient as in the test above, and the checkpoint's way back."""
+    B, (rows, d) = 2, LONG
+    T = rows // B
+    z, dy = long_rows(), long_rows()
+    packed, back = torch.empty(F.flashdp_checkpoint8_bytes(rows, d), dtype=torch.uint8, device=DEV), torch.empty_like(z)
+    F.flashdp_checkpoint8_pack(z, rows, d, F.BF16, packed)
+    F.flashdp_checkpoint8_unpack(packed, rows, d, F.BF16, back)
+    torch.cuda.synchronize()
+    assert torch.equal(back[LOOK].cpu().double(), quantise(z[LOOK].cpu().double(), False)[2])
+    dz, g, n = z, torch.empty(d, device=DEV), torch.empty(B, device=DEV)
+    F.flashdp_activation_dp_grad(dy, packed, True, B, T, d, F.BF16, "relu", 1e6, 0.0, 0, 0, dz, g, n)
+    torch.cuda.synchronize()
+    total, size = torch.zeros(d, device=DEV, dtype=torch.float64), torch.zeros(d, device=DEV, dtype=torch.float64)
+    for k in range(0, rows, 50000):
+        want = torch.where(back[k:k + 50000] > 0, dy[k:k + 50000], torch.zeros((), dtype=dy.dtype, device=DEV))
+        assert torch.equal(dz[k:k + 50000], want), k
+        total += want.double().sum(0)
+        size += want.double().abs().sum(0)
+    assert bool(((g.double() - total).abs() <= 2.0 ** -12 * size).all())
