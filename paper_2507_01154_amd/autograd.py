@@ -82,12 +82,14 @@ def _grad_call(packed, room):
     return call
 
 
-def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module, room=False):
+def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module, incoming, room=False):
     """The weight's gradient, now or - inside deferred_weight_grads, where None is returned - in the block call at its end.  X is the
-    activation [B, T, d_in], or with `packed` its 8-bit checkpoint."""
+    activation [B, T, d_in], or with `packed` its 8-bit checkpoint.  incoming: the tensor that autograd handed to the backward pass.  dY may be
+    another view of its memory, which autograd does not count: it would give an incoming gradient that nobody else holds to a leaf as its .grad
+    and add the next pass's to it in place.  So the record holds that very tensor as well."""
     pending = deferred_weight_grads._active
     if pending is not None:   # hand the layer to the per-block call made when the context exits
-        pending.pending.append(dict(X=X, packed=packed, dY=dY, B=B, T=T, weight=weight, C=C, sigma=sigma, seed=seed, layer=layer,
+        pending.pending.append(dict(X=X, packed=packed, dY=dY, incoming=incoming, B=B, T=T, weight=weight, C=C, sigma=sigma, seed=seed, layer=layer,
                                     norms=norms, add_noise=add_noise, module=module))
         return None
     d_out, d_in = weight.shape
@@ -120,7 +122,7 @@ class _DPLinearFn(torch.autograd.Function):
             dys = dys.to(xs.dtype)
         norms = norms_out if norms_out is not None else torch.empty((B,), dtype=torch.float32, device=x.device)
         grad_x = torch.matmul(dy, weight) if ctx.needs_input_grad[0] else None
-        grad_w = _weight_grad(xs, False, dys, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module)
+        grad_w = _weight_grad(xs, False, dys, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module, dy)
         return (grad_x, grad_w) + nothing
 
 
@@ -193,7 +195,7 @@ class _DPLinearEpilogueFn(torch.autograd.Function):
                 grad_x = torch.matmul(dz, weight)
             if need_w:
                 grad_w = _weight_grad(kept if eight else kept.reshape(B, T, d_in), eight, dz.reshape(B, T, d_out), B, T, weight, float(C), float(sigma),
-                                      seed, layer, schedule, norms, add_noise, module, room=True)
+                                      seed, layer, schedule, norms, add_noise, module, dy, room=True)
         return grad_x, grad_w, grad_b, dy if need_r else None, None, None, None, None, None
 
 

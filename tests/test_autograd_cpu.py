@@ -1,0 +1,81 @@
+"""The modules' glue on the CPU: what is recorded, deferred, refused and handed on, with the library's calls replaced by the
+formulas in torch.  The library's own arithmetic is tested on the GPU."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2507_01154_amd import autograd as A
+
+
+def clipped(G, C):
+    """sum_i G_i / max(1, |G_i| / C) and the norms, of per-sample gradients G [B, ...]."""
+    n = G.reshape(G.shape[0], -1).norm(dim=1)
+    return (G / (n / C).clamp(min=1.0).reshape(-1, *(1,) * (G.dim() - 1))).sum(0), n
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """The calls that the modules make, in torch, without noise, activations or 8-bit forms.  `calls` lists the block calls: layers and noise flag."""
+    calls = []
+
+    def linear_forward(X, W, bias, residual, rows, d_in, d_out, dtype, activation, Y, Z=None, z_8bit=False, stream=None):
+        y = X.reshape(rows, d_in) @ W.t()
+        y = y if bias is None else y + bias
+        Y.reshape(rows, d_out).copy_(y if residual is None else y + residual.reshape(rows, d_out))
+
+    def activation_grad(dY, Z, z_8bit, B, T, d_out, dtype, activation, C, sigma, seed, layer, dZ, out_grad, out_norms=None, workspace=None, stream=None,
+                        accumulate=False, add_noise=True):
+        g, n = clipped(dY.reshape(B, T, d_out).sum(1), C)
+        out_grad.copy_(g)
+        out_norms.copy_(n)
+
+    def block(layers, B, T, dtype, schedule="auto", workspace=None, stream=None, accumulate=False, add_noise=True):
+        calls.append((len(layers), add_noise))
+        for L in layers:
+            G = L["dY"].reshape(B, T, -1).transpose(1, 2) @ L["X"].reshape(B, T, -1)
+            g, n = clipped(G, L["C"])
+            L["out_grad"].copy_(g)
+            if L["out_norms"] is not None:
+                L["out_norms"].copy_(n)
+
+    def norm_forward(X, gamma, beta, rows, d, dtype, eps, Y, mean=None, rstd=None, stream=None):
+        Y.copy_(torch.nn.functional.layer_norm(X, (d,), gamma, beta, eps))
+
+    def norm_grad(X, dY, gamma, mean, rstd, B, T, d, dtype, C, sigma, seed, layer, dX, out_grad, out_norms=None, bias=True, workspace=None, stream=None,
+                  accumulate=False, add_noise=True):
+        out_grad.zero_()
+        if dX is not None:
+            dX.copy_(dY)
+
+    for name, f in (("flashdp_linear_forward", linear_forward), ("flashdp_activation_dp_grad", activation_grad), ("flashdp_block_dp_grad_micro", block),
+                    ("flashdp_layernorm_forward", norm_forward), ("flashdp_layernorm_dp_grad", norm_grad)):
+        monkeypatch.setattr(A.F, name, f)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    return calls
+
+
+def linear(d_in=6, d_out=4, **kw):
+    torch.manual_seed(3)
+    return A.DPLinear(d_in, d_out, **dict(dict(C=1.0, sigma=0.0, device="cpu", dtype=torch.float32, auto_step=False), **kw))
+
+
+@pytest.mark.parametrize("bias", [False, True])
+def test_a_leaf_residual_and_two_backward_passes_inside_one_deferred_context(library, bias):
+    """The output's gradient goes to the residual as it is, and is a deferred layer's dY: adding to residual.grad must not reach it."""
+    torch.manual_seed(1)
+    xs, dys = [torch.randn(3, 5, 6) for _ in range(2)], [torch.randn(3, 5, 4) for _ in range(2)]
+    got = []
+    for deferred in (False, True):
+        lin, r = linear(bias=bias), torch.randn(3, 5, 4, generator=torch.Generator().manual_seed(2)).requires_grad_()
+        with A.deferred_weight_grads() if deferred else contextlib.nullcontext():
+            for x, dy in zip(xs, dys):
+                # (clone: the passes' gradients are made on their way, as they are inside a model, and nobody else holds them)
+                (lin(x, residual=r) * 2.0).backward(dy.clone())
+            r.grad.mul_(3.0)
+        got.append([r.grad, lin.weight.grad] + ([lin.bias.grad] if bias else []))
+    for a, b in zip(*got):
+        assert torch.allclose(a, b, rtol=1e-6, atol=1e-6)
+    want = sum(clipped((2.0 * dy).transpose(1, 2) @ x, 1.0)[0] for x, dy in zip(xs, dys))
+    assert torch.allclose(got[1][1], want, rtol=1e-5, atol=1e-5)
