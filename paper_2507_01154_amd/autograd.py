@@ -23,7 +23,8 @@ class deferred_weight_grads:
     recorded layers go to the library in ONE flashdp_block_dp_grad call per (B, T, dtype) group, so that the
     per-block schedule applies (the aggregation of one layer running beside the contraction of the next)
     instead of one isolated call per layer.  The weights' .grad fields are filled (or added to) on exit.  The
-    price is that X and dY of every recorded layer stay alive until then."""
+    price is that X and dY of every recorded layer stay alive until then; one that has been written in place by then is an
+    error, as it is for what autograd saves."""
 
     _active = None
 
@@ -39,13 +40,18 @@ class deferred_weight_grads:
 
     def __exit__(self, exc_type, exc, tb):
         deferred_weight_grads._active = None
-        if exc_type is None:
-            self.flush()
-        self.pending = []
+        try:
+            if exc_type is None:
+                self.flush()
+        finally:
+            self.pending = []
         return False
 
     def flush(self):
         groups = {}
+        for rec in self.pending:
+            if _versions(rec["X"], rec["dY"]) != rec["versions"]:
+                raise RuntimeError("the input or the output gradient of a layer was modified in place before the deferred weight gradients were computed")
         for rec in self.pending:
             groups.setdefault((rec["B"], rec["T"], rec["dY"].dtype, rec["packed"]), []).append(rec)
         for (B, T, _, packed), recs in groups.items():
@@ -66,6 +72,11 @@ class deferred_weight_grads:
                 g = r["out"].to(r["weight"].dtype)
                 r["weight"].grad = g if r["weight"].grad is None else r["weight"].grad + g
         self.pending = []
+
+
+def _versions(*tensors):
+    """How often their memory was written in place (not counted for tensors made in inference mode)."""
+    return tuple(0 if t.is_inference() else t._version for t in tensors)
 
 
 def _grad_call(packed, room):
@@ -89,8 +100,8 @@ def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, n
     and add the next pass's to it in place.  So the record holds that very tensor as well."""
     pending = deferred_weight_grads._active
     if pending is not None:   # hand the layer to the per-block call made when the context exits
-        pending.pending.append(dict(X=X, packed=packed, dY=dY, incoming=incoming, B=B, T=T, weight=weight, C=C, sigma=sigma, seed=seed, layer=layer,
-                                    norms=norms, add_noise=add_noise, module=module))
+        pending.pending.append(dict(X=X, packed=packed, dY=dY, incoming=incoming, versions=_versions(X, dY), B=B, T=T, weight=weight, C=C, sigma=sigma,
+                                    seed=seed, layer=layer, norms=norms, add_noise=add_noise, module=module))
         return None
     d_out, d_in = weight.shape
     grad_w = torch.empty((d_out, d_in), dtype=torch.float32, device=dY.device)

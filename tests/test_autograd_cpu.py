@@ -79,3 +79,22 @@ def test_a_leaf_residual_and_two_backward_passes_inside_one_deferred_context(lib
         assert torch.allclose(a, b, rtol=1e-6, atol=1e-6)
     want = sum(clipped((2.0 * dy).transpose(1, 2) @ x, 1.0)[0] for x, dy in zip(xs, dys))
     assert torch.allclose(got[1][1], want, rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("epilogue", [False, True])
+@pytest.mark.parametrize("which", ["input", "gradient"])
+def test_what_a_deferred_layer_was_recorded_with_is_not_written_before_the_context_ends(library, which, epilogue):
+    """As autograd does for what it saves: a buffer that the next micro-batch is copied into would give gradients of the wrong samples."""
+    lin, x, dy = linear(bias=epilogue), torch.randn(3, 5, 6), torch.randn(3, 5, 4)
+    with pytest.raises(RuntimeError, match="in place"):
+        with A.deferred_weight_grads():
+            lin(x).backward(dy)
+            (x if which == "input" else dy).normal_()
+    assert lin.weight.grad is None and library == []
+    with A.deferred_weight_grads():          # and the next context starts empty
+        lin(x).backward(dy)
+    assert library == [(1, True)] and torch.allclose(lin.weight.grad, clipped(dy.transpose(1, 2) @ x, 1.0)[0], rtol=1e-5, atol=1e-6)
+    with A.deferred_weight_grads():          # afterwards they are the caller's
+        lin(x).backward(dy)
+    x.zero_()
+    dy.zero_()
