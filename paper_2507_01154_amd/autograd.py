@@ -20,7 +20,7 @@ from . import binding as F
 
 class deferred_weight_grads:
     """Context manager: DPLinear backward passes inside it only record (X, dY) of their layer; on exit all
-    recorded layers go to the library in ONE flashdp_block_dp_grad call per (B, T, dtype) group, so that the
+    recorded layers go to the library in ONE flashdp_block_dp_grad call per (device, B, T, dtype) group, so that the
     per-block schedule applies (the aggregation of one layer running beside the contraction of the next)
     instead of one isolated call per layer.  The weights' .grad fields are filled (or added to) on exit.  The
     price is that X and dY of every recorded layer stay alive until then; one that has been written in place by then is an
@@ -53,25 +53,29 @@ class deferred_weight_grads:
             if _versions(rec["X"], rec["dY"]) != rec["versions"]:
                 raise RuntimeError("the input or the output gradient of a layer was modified in place before the deferred weight gradients were computed")
         for rec in self.pending:
-            groups.setdefault((rec["B"], rec["T"], rec["dY"].dtype, rec["packed"]), []).append(rec)
-        for (B, T, _, packed), recs in groups.items():
-            grad = _grad_call(packed, packed)
-            layers = []
-            for r in recs:
-                r["out"] = torch.empty(r["weight"].shape, dtype=torch.float32, device=r["X"].device)
-                layers.append(dict(X=r["X"], dY=r["dY"], d_in=r["weight"].shape[1], d_out=r["weight"].shape[0], C=r["C"],
-                                   sigma=r["sigma"], seed=r["seed"], layer=r["layer"], out_grad=r["out"], out_norms=r["norms"]))
-            # layers of one group share the noise flag only if they agree; otherwise one call per flag value
-            for flag in sorted({r["add_noise"] for r in recs}, reverse=True):
-                sub = [L for L, r in zip(layers, recs) if r["add_noise"] == flag]
-                grad(sub, B, T, F.dtype_code(recs[0]["dY"]), self.schedule, accumulate=False, add_noise=flag)
-            for r in recs:
-                if r["module"] is not None and r["module"].keep_fp32_grad:
-                    m = r["module"]
-                    m.grad_fp32 = r["out"].clone() if m.grad_fp32 is None else m.grad_fp32 + r["out"]
-                g = r["out"].to(r["weight"].dtype)
-                r["weight"].grad = g if r["weight"].grad is None else r["weight"].grad + g
+            groups.setdefault((rec["X"].device, rec["B"], rec["T"], rec["dY"].dtype, rec["packed"]), []).append(rec)
+        for (device, B, T, _, packed), recs in groups.items():
+            with torch.cuda.device(device):
+                self._flush_group(recs, B, T, packed)
         self.pending = []
+
+    def _flush_group(self, recs, B, T, packed):
+        grad = _grad_call(packed, packed)
+        layers = []
+        for r in recs:
+            r["out"] = torch.empty(r["weight"].shape, dtype=torch.float32, device=r["X"].device)
+            layers.append(dict(X=r["X"], dY=r["dY"], d_in=r["weight"].shape[1], d_out=r["weight"].shape[0], C=r["C"],
+                               sigma=r["sigma"], seed=r["seed"], layer=r["layer"], out_grad=r["out"], out_norms=r["norms"]))
+        # layers of one group share the noise flag only if they agree; otherwise one call per flag value
+        for flag in sorted({r["add_noise"] for r in recs}, reverse=True):
+            sub = [L for L, r in zip(layers, recs) if r["add_noise"] == flag]
+            grad(sub, B, T, F.dtype_code(recs[0]["dY"]), self.schedule, accumulate=False, add_noise=flag)
+        for r in recs:
+            if r["module"] is not None and r["module"].keep_fp32_grad:
+                m = r["module"]
+                m.grad_fp32 = r["out"].clone() if m.grad_fp32 is None else m.grad_fp32 + r["out"]
+            g = r["out"].to(r["weight"].dtype)
+            r["weight"].grad = g if r["weight"].grad is None else r["weight"].grad + g
 
 
 def _versions(*tensors):

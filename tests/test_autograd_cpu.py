@@ -98,3 +98,17 @@ def test_what_a_deferred_layer_was_recorded_with_is_not_written_before_the_conte
         lin(x).backward(dy)
     x.zero_()
     dy.zero_()
+
+
+def test_deferred_layers_of_two_devices_go_to_two_calls_each_on_its_own_device(library, monkeypatch):
+    """Equal shapes on two devices ("meta" standing for the second): the library works on the current device."""
+    entered = []
+    monkeypatch.setattr(torch.cuda, "device", lambda d: entered.append(torch.device(d).type) or contextlib.nullcontext())
+    layers = [linear(), linear(device="meta"), linear()]
+    with A.deferred_weight_grads():
+        for lin in layers:
+            x = torch.ones(3, 5, 6, device=lin.weight.device)
+            lin(x).backward(torch.ones(3, 5, 4, device=x.device))
+        del entered[:]
+    assert library == [(2, True), (1, True)] and entered == ["cpu", "meta"]
+    assert all(lin.weight.grad.device == lin.weight.device for lin in layers) and torch.equal(layers[0].weight.grad, layers[2].weight.grad)
