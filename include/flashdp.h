@@ -22,7 +22,9 @@
  *     e = d * d_in + p,  g = e >> 2,
  * uniforms u(r) = ((r >> 8) + 0.5) * 2^-24, pairs (r0,r1) -> (z0,z1) = rho*(cos,sin)(2 pi u(r1)),
  * rho = sqrt(-2 ln u(r0)), and (r2,r3) -> (z2,z3) likewise.  Same (seed, layer) => same noise:
- * the caller must fold the training step into seed, or noise repeats across steps.
+ * the caller must fold the training step into seed, or noise repeats across steps.  seed is passed by value: a call that is
+ * captured into a HIP graph repeats its noise in every replay, so replayed steps take add_noise = 0 (or sigma = 0) and their
+ * noise from a call outside the graph.
  *
  * Conventions for every entry point
  *   - All data pointers are DEVICE pointers (HIP, current device) owned by the caller.

@@ -52,6 +52,7 @@ class deferred_weight_grads:
         for rec in self.pending:
             if _versions(rec["X"], rec["dY"]) != rec["versions"]:
                 raise RuntimeError("the input or the output gradient of a layer was modified in place before the deferred weight gradients were computed")
+            _check_capture(rec["module"], rec["sigma"], rec["add_noise"])
         for rec in self.pending:
             groups.setdefault((rec["X"].device, rec["B"], rec["T"], rec["dY"].dtype, rec["packed"]), []).append(rec)
         for (device, B, T, _, packed), recs in groups.items():
@@ -83,6 +84,14 @@ def _versions(*tensors):
     return tuple(0 if t.is_inference() else t._version for t in tensors)
 
 
+def _check_capture(module, sigma, add_noise):
+    """What a graph keeps of a call is the seed's value, so every replay adds the same noise.  A module that counts its steps by itself has
+    promised another field for each of them, and does not have its noise captured."""
+    if module is not None and module.auto_step and add_noise and sigma > 0 and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("a graph's replays would repeat the noise of its capture: capture with add_noise = False (or sigma = 0) and add the noise outside "
+                           "the graph, or set auto_step = False, which leaves steps and seeds to the caller")
+
+
 def _grad_call(packed, room):
     """The block call for activations as they are, or for 8-bit checkpoints of them.  Both take the library's workspace; with `room`, while a
     graph is being captured, one of torch's, which the graph keeps."""
@@ -107,6 +116,7 @@ def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, n
         pending.pending.append(dict(X=X, packed=packed, dY=dY, incoming=incoming, versions=_versions(X, dY), B=B, T=T, weight=weight, C=C, sigma=sigma,
                                     seed=seed, layer=layer, norms=norms, add_noise=add_noise, module=module))
         return None
+    _check_capture(module, sigma, add_noise)
     d_out, d_in = weight.shape
     grad_w = torch.empty((d_out, d_in), dtype=torch.float32, device=dY.device)
     L = [dict(X=X, dY=dY, d_in=d_in, d_out=d_out, C=C, sigma=sigma, seed=seed, layer=layer, out_grad=grad_w, out_norms=norms)]
@@ -191,6 +201,8 @@ class _DPLinearEpilogueFn(torch.autograd.Function):
         need_x, need_w, need_b, need_r = ctx.needs_input_grad[:4]
         d_out, d_in = weight.shape
         grad_x = grad_w = grad_b = None
+        if need_b:
+            _check_capture(module, sigma, add_noise)
         with torch.cuda.device(dy.device):
             dys = _dense(dy.to(weight.dtype))
             dz = dys
@@ -221,6 +233,9 @@ class _DPModule(torch.nn.Module):
     auto_step (the default) it advances by itself at every forward pass whose backward adds noise, so that two
     optimizer steps never receive the same field - the Gaussian mechanism of Algorithm 1 would be void otherwise
     (the difference of two updates would be noise-free).  last_seed is the seed the last forward pass used.
+    A backward pass captured into a graph keeps its seed: every replay adds the same field.  With auto_step a backward pass that
+    adds noise therefore refuses to be captured; without, the noise is that of `step` as the caller has set it, and a graph's is that of
+    the capture for good - replays are steps of one mechanism only where the caller adds fresh noise outside the graph.
     Gradient accumulation over micro-batches (Appendix D.1): set add_noise = False for all micro-batches of a step but
     the last; every micro-batch is clipped per sample, torch sums the clipped sums in .grad, and the noise goes
     in once, with the last micro-batch (the step then advances once, too).
@@ -323,6 +338,8 @@ class _DPLayerNormFn(torch.autograd.Function):
             dx = torch.empty_like(xs) if need_x else None
             # weight and bias are one vector with one norm, whichever of them is wanted
             need_g = need_w or need_b
+            if need_g:
+                _check_capture(module, sigma, add_noise)
             g = torch.empty((2 if has_bias else 1, d), dtype=torch.float32, device=dy.device) if need_g else None
             ws = _workspace(F.flashdp_layernorm_workspace_bytes(B, T, d, code, has_bias), dy.device) if need_g else None
             if need_x or need_g:

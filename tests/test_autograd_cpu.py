@@ -112,3 +112,44 @@ def test_deferred_layers_of_two_devices_go_to_two_calls_each_on_its_own_device(l
         del entered[:]
     assert library == [(2, True), (1, True)] and entered == ["cpu", "meta"]
     assert all(lin.weight.grad.device == lin.weight.device for lin in layers) and torch.equal(layers[0].weight.grad, layers[2].weight.grad)
+
+
+def test_a_graph_does_not_capture_noise_that_its_replays_would_repeat(library, monkeypatch):
+    """The step advances in Python and the seed goes by value, so a replay would add the field of the capture again.  Modules that promise another
+    field every step refuse; without noise, or with the step left to the caller, they are captured."""
+    def backward(m):
+        x = torch.randn(3, 5, 6)
+        m(x).backward(torch.randn(3, 5, m.weight.shape[0]))
+
+    norm = lambda **kw: A.DPLayerNorm(6, device="cpu", dtype=torch.float32, **kw)      # noqa: E731
+    makers = [lambda **kw: linear(**kw), lambda **kw: linear(bias=True, **kw), norm]
+    for make in makers:
+        refused, quiet, by_hand, micro = make(sigma=0.5, auto_step=True), make(sigma=0.0, auto_step=True), make(sigma=0.5, auto_step=False), make(sigma=0.5, auto_step=True)
+        micro.add_noise = False
+        for capturing in (False, True):
+            monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+            for m in (quiet, by_hand, micro):
+                backward(m)
+            if not capturing:
+                backward(refused)
+                continue
+            for p in refused.parameters():
+                p.grad = None
+            with pytest.raises(RuntimeError, match="replay"):
+                backward(refused)
+            assert all(p.grad is None for p in refused.parameters())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    frozen = linear(sigma=0.5, auto_step=True, bias=True)      # no parameter of it is trained: no noise
+    for p in frozen.parameters():
+        p.requires_grad_(False)
+    x = torch.randn(3, 5, 6, requires_grad=True)
+    frozen(x).backward(torch.ones(3, 5, 4))
+    lin = linear(sigma=0.5, auto_step=True)
+    with pytest.raises(RuntimeError, match="replay"):
+        with A.deferred_weight_grads():
+            backward(lin)
+    assert lin.weight.grad is None
+    with A.deferred_weight_grads():      # recorded in the capture, computed after it: once
+        backward(lin)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    assert lin.weight.grad is not None

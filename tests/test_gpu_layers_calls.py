@@ -1,0 +1,29 @@
+"""Calls around the weight gradient that the other files do not make: noise inside a capture, schedules of several layers on
+checkpoints, sums over many samples, single products, rows that decide a result alone."""
+import pytest
+import torch
+
+import paper_2507_01154_amd as F
+from gpu_util import DEV, env
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_module_that_counts_its_steps_does_not_have_its_noise_captured():
+    from paper_2507_01154_amd.autograd import DPLinear
+    make = lambda **kw: DPLinear(64, 48, C=1.0, bias=True, schedule="twopass", device=DEV, **kw)     # noqa: E731
+    refused, quiet = make(sigma=0.5), make(sigma=0.0)
+    x, dy, total = torch.randn(2, 9, 64, device=DEV).bfloat16(), torch.randn(2, 9, 48, device=DEV).bfloat16(), torch.zeros(1, device=DEV)
+    warm = make(sigma=0.0)               # (kernels are launched eagerly once, by a module that is not captured)
+    want = [t.clone() for t in torch.autograd.grad(warm(x), list(warm.parameters()), dy)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError, match="replay"):
+            torch.autograd.grad(refused(x), list(refused.parameters()), dy)
+        got = torch.autograd.grad(quiet(x), list(quiet.parameters()), dy)
+        total.add_(1.0)                  # the capture goes on
+    for rep in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(total) == rep + 1 and all(torch.equal(a, b) for a, b in zip(got, want))
