@@ -586,6 +586,15 @@ int resolve_schedule(int schedule) {
   return forced >= 0 ? forced : schedule;
 }
 
+// What a schedule asks of the sizes beyond check_dims.
+int check_schedule(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule) {
+  for (int l = 0; schedule == FLASHDP_SCHEDULE_GHOST && l < n_layers; ++l) {   // grid of the Gram kernel
+    const int64_t nb = gram_blocks(T, layers[l].d_in, layers[l].d_out, dtype);
+    if (nb > 32768 || nb * (nb + 1) / 2 * B >= (int64_t(1) << 31)) return FLASHDP_UNSUPPORTED_SHAPE;   // 32-bit block arithmetic
+  }
+  return FLASHDP_OK;
+}
+
 // The single-launch form needs a workgroup per 256 x 256 tile resident at the same time (one per CU: its ring takes
 // most of a CU's LDS), 16-bit inputs on the matrix-core path, and clip factors for all samples in LDS.
 bool fused_ok(int64_t B, int64_t T, int64_t P, int64_t D, int dtype, int cus) {
@@ -1131,6 +1140,10 @@ int library_workspace(size_t need, hipStream_t stream, void** ptr) {
   size_t got = 0;
   return owned_workspace(need, ptr, &got);
 }
+int schedule_of_call(int schedule) { return resolve_schedule(schedule); }
+int check_schedule_sizes(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule) {
+  return check_schedule(layers, n_layers, B, T, dtype, schedule);
+}
 int64_t compute_units() { return plan_cus(); }
 int forward_override() { return env().forward; }
 void note_kernel(const char* name) { g_ctx.last_kernel = name; }
@@ -1158,13 +1171,11 @@ int flashdp_block_dp_grad_micro(const flashdp_layer_t* layers, int n_layers, int
     need_small = std::max(need_small, layer_ws_bytes(layers[l], B, T, dtype, FLASHDP_SCHEDULE_TWOPASS));
     need_explicit = std::max(need_explicit, layer_ws_bytes(layers[l], B, T, dtype, FLASHDP_SCHEDULE_EXPLICIT));
     need_ghost = std::max(need_ghost, layer_ws_bytes(layers[l], B, T, dtype, FLASHDP_SCHEDULE_GHOST));
-    if (schedule == FLASHDP_SCHEDULE_GHOST) {   // grid of the Gram kernel
-      const int64_t nb = gram_blocks(T, layers[l].d_in, layers[l].d_out, dtype);
-      if (nb > 32768 || nb * (nb + 1) / 2 * B >= (int64_t(1) << 31)) return FLASHDP_UNSUPPORTED_SHAPE;   // 32-bit block arithmetic
-    }
   }
+  int st = check_schedule(layers, n_layers, B, T, dtype, schedule);
+  if (st != FLASHDP_OK) return st;
   int dev = 0;
-  int st = device_or_error(&dev);
+  st = device_or_error(&dev);
   if (st != FLASHDP_OK) return st;
   // The overlapped schedule needs two work items or more (layers, or sample chunks of a layer), 16-bit inputs on
   // the large-tile matrix-core path (where the aggregation is worth hiding) and the full stage mask; otherwise it is

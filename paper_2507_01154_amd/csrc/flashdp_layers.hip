@@ -523,7 +523,7 @@ static size_t unpacked_bytes(const flashdp_layer_t* layers, int n_layers, int64_
 }
 
 size_t flashdp_workspace_bytes_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule) {
-  const size_t need = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, schedule);
+  const size_t need = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, api::schedule_of_call(schedule));
   for (int l = 0; need != 0 && l < n_layers; ++l)
     if (check_samples(B, T, layers[l].d_in) != FLASHDP_OK) return 0;
   return need == 0 ? 0 : unpacked_bytes(layers, n_layers, B, T, dtype) + need;
@@ -543,14 +543,17 @@ int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layer
   for (int l = 0; l < n_layers; ++l)
     if (layers[l].d_in <= 0 || layers[l].d_out <= 0) return FLASHDP_INVALID_ARGUMENT;
   for (int l = 0; l < n_layers; ++l)
-    if (check_samples(B, T, layers[l].d_in) != FLASHDP_OK) return FLASHDP_UNSUPPORTED_SHAPE;
+    if (check_samples(B, T, layers[l].d_in) != FLASHDP_OK || checkpoint8_grid(checkpoint8_chunks(B * T, layers[l].d_in, dtype)) > GRID_LIMIT)
+      return FLASHDP_UNSUPPORTED_SHAPE;
+  schedule = api::schedule_of_call(schedule);
   const size_t inner = flashdp_workspace_bytes(layers, n_layers, B, T, dtype, schedule);
   if (inner == 0) return FLASHDP_UNSUPPORTED_SHAPE;
+  int st = api::check_schedule_sizes(layers, n_layers, B, T, dtype, schedule);
+  if (st != FLASHDP_OK) return st;
   const size_t room = unpacked_bytes(layers, n_layers, B, T, dtype);
   if (workspace && workspace_bytes < room + inner) return FLASHDP_WORKSPACE_TOO_SMALL;
   int dev = 0;
-  int st = api::current_device(&dev);
-  if (st != FLASHDP_OK) return st;
+  if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (!workspace) {
     if ((st = api::library_workspace(room + inner, hs, &workspace)) != FLASHDP_OK) return st;

@@ -27,3 +27,27 @@ def test_a_module_that_counts_its_steps_does_not_have_its_noise_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert float(total) == rep + 1 and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def packed_and_back(x, rows, d, code):
+    p, y = torch.empty(F.flashdp_checkpoint8_bytes(rows, d), dtype=torch.uint8, device=DEV), torch.empty_like(x)
+    F.flashdp_checkpoint8_pack(x, rows, d, code, p)
+    F.flashdp_checkpoint8_unpack(p, rows, d, code, y)
+    return p, y
+
+
+def gradients(call, X, dYs, B, T, P, code, schedule, workspace=None):
+    layers = [dict(X=X, dY=dY, d_in=P, d_out=dY.shape[-1], C=1.0 + k, sigma=0.5, seed=7, layer=k, out_grad=torch.empty(dY.shape[-1], P, device=DEV),
+                   out_norms=torch.empty(B, device=DEV)) for k, dY in enumerate(dYs)]
+    call(layers, B, T, code, schedule, workspace)
+    torch.cuda.synchronize()
+    return [t for L in layers for t in (L["out_grad"], L["out_norms"])], F.flashdp_last_schedule()
+
+
+def test_the_schedule_that_replaces_the_argument_has_its_workspace():
+    x, dYs = torch.randn(8 * 64, 512, device=DEV).bfloat16(), [torch.randn(8, 64, 256, device=DEV).bfloat16()]
+    p, y = packed_and_back(x, 8 * 64, 512, F.BF16)
+    want, _ = gradients(F.flashdp_block_dp_grad_micro, y, dYs, 8, 64, 512, F.BF16, "scratch")
+    with env(FLASHDP_SCHEDULE="scratch"):
+        got, how = gradients(F.flashdp_block_dp_grad_checkpoint8, p, dYs, 8, 64, 512, F.BF16, "twopass")
+    assert how == "scratch" and all(torch.equal(a, b) for a, b in zip(got, want))
