@@ -298,8 +298,12 @@ int flashdp_checkpoint8_pack(const void* X, int64_t rows, int64_t d, int dtype, 
 int flashdp_checkpoint8_unpack(const void* packed, int64_t rows, int64_t d, int dtype, void* X, void* stream);
 
 /* flashdp_block_dp_grad_micro with every layer's X an 8-bit checkpoint of its [B * T][d_in] activation: each is unpacked to `dtype`
- * into the workspace (layers in a row with the same X once) and contracted from there, so the memory of one layer's activation is
- * needed at a time instead of all layers'.  Same schedules and results as unpacking by hand.  Workspace: flashdp_workspace_bytes_checkpoint8. */
+ * into the workspace and contracted from there, so the memory of one layer's activation is needed at a time instead of all
+ * layers'.  Layers in a row with the same X (16 at most) are unpacked once and go to one call of flashdp_block_dp_grad_micro: schedule
+ * and results are that call's on the unpacked activation, with a null workspace or one of that much less than the caller's.  Layers of
+ * different X follow each other as calls of their own, so nothing of theirs overlaps or shares a launch (and the order of additions of
+ * short sequences, which are formed in groups, can differ from that of one call for all).
+ * Workspace: flashdp_workspace_bytes_checkpoint8. */
 int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule, void* workspace,
                                       size_t workspace_bytes, void* stream, int accumulate, int add_noise);
 size_t flashdp_workspace_bytes_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule);

@@ -22,7 +22,8 @@ class deferred_weight_grads:
     """Context manager: DPLinear backward passes inside it only record (X, dY) of their layer; on exit all
     recorded layers go to the library in ONE flashdp_block_dp_grad call per (device, B, T, dtype) group, so that the
     per-block schedule applies (the aggregation of one layer running beside the contraction of the next)
-    instead of one isolated call per layer.  The weights' .grad fields are filled (or added to) on exit.  The
+    instead of one isolated call per layer (layers with 8-bit checkpoints go together too, but are computed one
+    after the other: each keeps a checkpoint of its own, and unpacks it in front of its contraction).  The weights' .grad fields are filled (or added to) on exit.  The
     price is that X and dY of every recorded layer stay alive until then; one that has been written in place by then is an
     error, as it is for what autograd saves."""
 

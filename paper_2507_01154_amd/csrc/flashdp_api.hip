@@ -59,7 +59,10 @@ thread_local Context g_ctx;
 
 struct OwnedWs { void* ptr = nullptr; size_t bytes = 0; };
 std::mutex g_ws_mutex;
-std::map<int, OwnedWs> g_owned;   // device -> library-owned workspace
+// device -> library-owned memory: the calls' workspace, and apart from it the activation that a call from 8-bit checkpoints unpacks (the
+// call it is passed on to takes the workspace as it always does)
+enum OwnedUse : int { OWNED_WORKSPACE = 0, OWNED_ACTIVATION = 1, OWNED_USES = 2 };
+std::map<int, OwnedWs> g_owned[OWNED_USES];
 
 // Per-device second stream and events of the overlapped schedule (default priority, created on first use).
 struct SideStream {
@@ -546,12 +549,13 @@ int device_or_error(int* dev) {
 
 // wish: the size to take, if more than need, when the workspace has to grow anyway.  least: what the caller on `stream` can do
 // with where the workspace must not grow, while a graph is captured (growing would end the capture).
-int owned_workspace(size_t need, void** ptr, size_t* bytes, size_t wish = 0, size_t least = SIZE_MAX, hipStream_t stream = nullptr) {
+int owned_workspace(size_t need, void** ptr, size_t* bytes, size_t wish = 0, size_t least = SIZE_MAX, hipStream_t stream = nullptr,
+                    OwnedUse use = OWNED_WORKSPACE) {
   int dev = 0;
   int st = device_or_error(&dev);
   if (st != FLASHDP_OK) return st;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
-  OwnedWs& w = g_owned[dev];
+  OwnedWs& w = g_owned[use][dev];
   if (w.bytes < need && w.bytes >= least) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
@@ -1132,14 +1136,18 @@ namespace flashdp {
 namespace api {
 
 int current_device(int* dev) { return device_or_error(dev); }
-int library_workspace(size_t need, hipStream_t stream, void** ptr) {
-  // (a graph would keep the address, and a later call that grows the workspace frees it)
+namespace {
+int owned_outside_graphs(size_t need, hipStream_t stream, void** ptr, OwnedUse use) {
+  // (a graph would keep the address, and a later call that grows the memory frees it)
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
   if (capture != hipStreamCaptureStatusNone) return FLASHDP_WORKSPACE_TOO_SMALL;
   size_t got = 0;
-  return owned_workspace(need, ptr, &got);
+  return owned_workspace(need, ptr, &got, 0, SIZE_MAX, nullptr, use);
 }
+}  // namespace
+int library_workspace(size_t need, hipStream_t stream, void** ptr) { return owned_outside_graphs(need, stream, ptr, OWNED_WORKSPACE); }
+int library_activation(size_t need, hipStream_t stream, void** ptr) { return owned_outside_graphs(need, stream, ptr, OWNED_ACTIVATION); }
 int schedule_of_call(int schedule) { return resolve_schedule(schedule); }
 int check_schedule_sizes(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule) {
   return check_schedule(layers, n_layers, B, T, dtype, schedule);
@@ -1676,12 +1684,14 @@ int flashdp_release(void) {
   std::lock_guard<std::mutex> lock(g_ws_mutex);
   int cur = 0;
   const bool have_cur = hipGetDevice(&cur) == hipSuccess;
-  for (auto& kv : g_owned) {
-    if (!kv.second.ptr) continue;
-    if (hipSetDevice(kv.first) != hipSuccess) continue;
-    (void)hipDeviceSynchronize();
-    (void)hipFree(kv.second.ptr);
-    kv.second = OwnedWs();
+  for (auto& owned : g_owned) {
+    for (auto& kv : owned) {
+      if (!kv.second.ptr) continue;
+      if (hipSetDevice(kv.first) != hipSuccess) continue;
+      (void)hipDeviceSynchronize();
+      (void)hipFree(kv.second.ptr);
+      kv.second = OwnedWs();
+    }
   }
   std::lock_guard<std::mutex> side_lock(g_side_mutex);
   for (auto& kv : g_side) {

@@ -555,11 +555,12 @@ int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layer
   int dev = 0;
   if ((st = api::current_device(&dev)) != FLASHDP_OK) return st;
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  if (!workspace) {
-    if ((st = api::library_workspace(room + inner, hs, &workspace)) != FLASHDP_OK) return st;
-    workspace_bytes = room + inner;
-  }
-  char* ws = static_cast<char*>(workspace);
+  // The activation, and the workspace of the ordinary call: what is left of the caller's, or none, so that it takes the library's as it
+  // does without checkpoints.
+  void* unpacked = workspace;
+  if (!workspace && (st = api::library_activation(room, hs, &unpacked)) != FLASHDP_OK) return st;
+  void* rest = workspace ? static_cast<char*>(workspace) + room : nullptr;
+  const size_t rest_bytes = workspace ? workspace_bytes - room : 0;
   // Layers in a row that share their activation (the projections of an attention block) are unpacked once and go to one call.
   constexpr int RUN = 16;
   for (int l = 0; l < n_layers;) {
@@ -567,12 +568,12 @@ int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layer
     int n = 0;
     while (l + n < n_layers && n < RUN && layers[l + n].X == layers[l].X && layers[l + n].d_in == layers[l].d_in) {
       run[n] = layers[l + n];
-      run[n].X = ws;
+      run[n].X = unpacked;
       ++n;
     }
-    st = flashdp_checkpoint8_unpack(layers[l].X, B * T, layers[l].d_in, dtype, ws, stream);
+    st = flashdp_checkpoint8_unpack(layers[l].X, B * T, layers[l].d_in, dtype, unpacked, stream);
     if (st == FLASHDP_OK)
-      st = flashdp_block_dp_grad_micro(run, n, B, T, dtype, schedule, ws + room, workspace_bytes - room, stream, accumulate, add_noise);
+      st = flashdp_block_dp_grad_micro(run, n, B, T, dtype, schedule, rest, rest_bytes, stream, accumulate, add_noise);
     if (st != FLASHDP_OK) return st;
     l += n;
   }

@@ -44,6 +44,24 @@ def gradients(call, X, dYs, B, T, P, code, schedule, workspace=None):
     return [t for L in layers for t in (L["out_grad"], L["out_norms"])], F.flashdp_last_schedule()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,T,P,Ds", [(8, 256, 2048, (2048, 1024, 2048)), (4, 16, 256, (256, 512)), (6, 1, 264, (512, 96)), (3, 200, 100, (33, 65)), (16, 64, 64, (64,) * 18)])
+@pytest.mark.parametrize("schedule", ["auto", "overlap", "scratch", "twopass"])
+def test_layers_on_one_checkpoint_take_the_schedule_that_they_take_on_the_unpacked_activation(schedule, B, T, P, Ds, dtype):
+    """With the library's memory, and with the caller's: the same schedule, and the same bits."""
+    torch.manual_seed(T)
+    x, dYs = torch.randn(B * T, P, device=DEV).to(dtype), [torch.randn(B, T, d, device=DEV).to(dtype) for d in Ds]
+    code = F.dtype_code(x)
+    p, y = packed_and_back(x, B * T, P, code)
+    room = (B * T * P * x.element_size() + 255) // 256 * 256
+    run = dYs[:16]           # (of 18 layers two go to a call of their own)
+    for nbytes in (None, F.flashdp_workspace_bytes([dict(X=None, dY=None, d_in=P, d_out=d, C=1.0, sigma=0.0, seed=0, layer=0, out_grad=None) for d in Ds], B, T, code, schedule)):
+        ws = lambda n: None if nbytes is None else torch.empty(max(n, 16), dtype=torch.uint8, device=DEV)       # noqa: E731
+        got, how = gradients(F.flashdp_block_dp_grad_checkpoint8, p, dYs, B, T, P, code, schedule, ws((nbytes or 0) + room))
+        want, by_hand = gradients(F.flashdp_block_dp_grad_micro, y, run, B, T, P, code, schedule, ws(nbytes or 0))
+        assert (how == by_hand or len(Ds) > 16) and all(torch.equal(a, b) for a, b in zip(got, want)), (nbytes, how, by_hand)
+
+
 def test_the_schedule_that_replaces_the_argument_has_its_workspace():
     x, dYs = torch.randn(8 * 64, 512, device=DEV).bfloat16(), [torch.randn(8, 64, 256, device=DEV).bfloat16()]
     p, y = packed_and_back(x, 8 * 64, 512, F.BF16)
@@ -51,3 +69,12 @@ def test_the_schedule_that_replaces_the_argument_has_its_workspace():
     with env(FLASHDP_SCHEDULE="scratch"):
         got, how = gradients(F.flashdp_block_dp_grad_checkpoint8, p, dYs, 8, 64, 512, F.BF16, "twopass")
     assert how == "scratch" and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_the_overlapped_schedule_is_taken_from_checkpoints_as_it_is_without_them():
+    B, T, P = 4, 1024, 4096
+    x, dYs = torch.randn(B * T, P, device=DEV).bfloat16(), [torch.randn(B, T, P, device=DEV).bfloat16() for _ in range(2)]
+    p, y = packed_and_back(x, B * T, P, F.BF16)
+    want, by_hand = gradients(F.flashdp_block_dp_grad_micro, y, dYs, B, T, P, F.BF16, "auto")
+    got, how = gradients(F.flashdp_block_dp_grad_checkpoint8, p, dYs, B, T, P, F.BF16, "auto")
+    assert by_hand == how == "overlap" and all(torch.equal(a, b) for a, b in zip(got, want))
