@@ -62,7 +62,7 @@ class deferred_weight_grads:
         self.pending = []
 
     def _flush_group(self, recs, B, T, packed):
-        grad = _grad_call(packed, packed)
+        grad = _grad_call(packed)
         layers = []
         for r in recs:
             r["out"] = torch.empty(r["weight"].shape, dtype=torch.float32, device=r["X"].device)
@@ -93,21 +93,24 @@ def _check_capture(module, sigma, add_noise):
                            "the graph, or set auto_step = False, which leaves steps and seeds to the caller")
 
 
-def _grad_call(packed, room):
-    """The block call for activations as they are, or for 8-bit checkpoints of them.  Both take the library's workspace; with `room`, while a
-    graph is being captured, one of torch's, which the graph keeps."""
+def _grad_call(packed):
+    """The block call for activations as they are, or for 8-bit checkpoints of them.  Both take the library's workspace, or, while a graph is
+    being captured, one of torch's: the graph keeps its memory, where the library's would be freed by a later call that makes it grow."""
     grad, size = ((F.flashdp_block_dp_grad_checkpoint8, F.flashdp_workspace_bytes_checkpoint8) if packed
                   else (F.flashdp_block_dp_grad_micro, F.flashdp_workspace_bytes))
-    if not room or not torch.cuda.is_current_stream_capturing():
+    if not torch.cuda.is_current_stream_capturing():
         return grad
 
     def call(layers, B, T, dtype, schedule, **kw):
-        grad(layers, B, T, dtype, schedule, _workspace(size(layers, B, T, dtype, schedule), layers[0]["X"].device), **kw)
+        room = schedule
+        if F.schedule_code(schedule) == F.SCHEDULE_AUTO:      # rows without a sequence park nothing; two layers or more can take turns in two slots
+            room = "twopass" if T == 1 and B > 1 else "overlap" if len(layers) > 1 else "scratch"
+        grad(layers, B, T, dtype, schedule, _workspace(size(layers, B, T, dtype, room), layers[0]["X"].device), **kw)
 
     return call
 
 
-def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module, incoming, room=False):
+def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, norms, add_noise, module, incoming):
     """The weight's gradient, now or - inside deferred_weight_grads, where None is returned - in the block call at its end.  X is the
     activation [B, T, d_in], or with `packed` its 8-bit checkpoint.  incoming: the tensor that autograd handed to the backward pass.  dY may be
     another view of its memory, which autograd does not count: it would give an incoming gradient that nobody else holds to a leaf as its .grad
@@ -121,7 +124,7 @@ def _weight_grad(X, packed, dY, B, T, weight, C, sigma, seed, layer, schedule, n
     d_out, d_in = weight.shape
     grad_w = torch.empty((d_out, d_in), dtype=torch.float32, device=dY.device)
     L = [dict(X=X, dY=dY, d_in=d_in, d_out=d_out, C=C, sigma=sigma, seed=seed, layer=layer, out_grad=grad_w, out_norms=norms)]
-    _grad_call(packed, room)(L, B, T, F.dtype_code(dY), schedule, accumulate=False, add_noise=add_noise)
+    _grad_call(packed)(L, B, T, F.dtype_code(dY), schedule, accumulate=False, add_noise=add_noise)
     if module is not None and module.keep_fp32_grad:
         module.grad_fp32 = grad_w.clone() if module.grad_fp32 is None else module.grad_fp32 + grad_w
     return grad_w.to(weight.dtype)
@@ -223,7 +226,7 @@ class _DPLinearEpilogueFn(torch.autograd.Function):
                 grad_x = torch.matmul(dz, weight)
             if need_w:
                 grad_w = _weight_grad(kept if eight else kept.reshape(B, T, d_in), eight, dz.reshape(B, T, d_out), B, T, weight, float(C), float(sigma),
-                                      seed, layer, schedule, norms, add_noise, module, dy, room=True)
+                                      seed, layer, schedule, norms, add_noise, module, dy)
         return grad_x, grad_w, grad_b, dy if need_r else None, None, None, None, None, None
 
 

@@ -14,10 +14,17 @@ def clipped(G, C):
     return (G / (n / C).clamp(min=1.0).reshape(-1, *(1,) * (G.dim() - 1))).sum(0), n
 
 
+class Calls(list):
+    def __init__(self):
+        super().__init__()
+        self.rooms = []
+
+
 @pytest.fixture
 def library(monkeypatch):
-    """The calls that the modules make, in torch, without noise, activations or 8-bit forms.  `calls` lists the block calls: layers and noise flag."""
-    calls = []
+    """The calls that the modules make, in torch, without noise, activations or 8-bit forms.  `calls` lists the block calls: layers and noise flag;
+    calls.rooms their workspaces."""
+    calls = Calls()
 
     def linear_forward(X, W, bias, residual, rows, d_in, d_out, dtype, activation, Y, Z=None, z_8bit=False, stream=None):
         y = X.reshape(rows, d_in) @ W.t()
@@ -32,6 +39,7 @@ def library(monkeypatch):
 
     def block(layers, B, T, dtype, schedule="auto", workspace=None, stream=None, accumulate=False, add_noise=True):
         calls.append((len(layers), add_noise))
+        calls.rooms.append(workspace)
         for L in layers:
             G = L["dY"].reshape(B, T, -1).transpose(1, 2) @ L["X"].reshape(B, T, -1)
             g, n = clipped(G, L["C"])
@@ -153,3 +161,27 @@ def test_a_graph_does_not_capture_noise_that_its_replays_would_repeat(library, m
         backward(lin)
         monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     assert lin.weight.grad is not None
+
+
+def test_a_captured_backward_pass_never_takes_the_librarys_workspace(library, monkeypatch):
+    """A graph keeps the addresses of its capture, and the library's workspace moves when a later call makes it grow: every kind of layer, alone or
+    deferred, brings memory of torch's, which the graph keeps, where it is captured."""
+    def pass_of(deferred, T):
+        with A.deferred_weight_grads() if deferred else contextlib.nullcontext():
+            for m in layers:
+                x = torch.randn(3, T, 6)
+                m(x, residual=torch.zeros(3, T, 4) if m.bias is not None else None).backward(torch.randn(3, T, 4))
+
+    layers = [linear(), linear(bias=True), linear()]
+    for capturing in (False, True):
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+        for deferred in (False, True):
+            for T in (1, 5):
+                del library[:], library.rooms[:]
+                pass_of(deferred, T)
+                assert [n for n, _ in library] == ([3] if deferred else [1, 1, 1])
+                assert all((r is not None) == capturing for r in library.rooms)
+                for r in library.rooms if capturing else []:
+                    # what any schedule needs at least; with a sequence, what the layers park in, twice where one can be summed beside the next
+                    size = lambda s: A.F.flashdp_workspace_bytes([dict(X=None, dY=None, d_in=6, d_out=4, C=1.0, sigma=0.0, seed=0, layer=0, out_grad=None)] * 3, 3, T, A.F.F32, s)   # noqa: E731
+                    assert r.numel() >= size("twopass" if T == 1 else "overlap" if deferred else "scratch")

@@ -78,3 +78,50 @@ def test_the_overlapped_schedule_is_taken_from_checkpoints_as_it_is_without_them
     want, by_hand = gradients(F.flashdp_block_dp_grad_micro, y, dYs, B, T, P, F.BF16, "auto")
     got, how = gradients(F.flashdp_block_dp_grad_checkpoint8, p, dYs, B, T, P, F.BF16, "auto")
     assert by_hand == how == "overlap" and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("deferred", [False, True])
+def test_captured_layers_without_an_epilogue_outlive_the_librarys_workspace(deferred, T):
+    """Replayed beside eager calls that make the library's workspace grow, and after it was given back.  The captured modules are never run eagerly."""
+    from contextlib import nullcontext
+    from paper_2507_01154_amd.autograd import DPLinear, deferred_weight_grads
+    torch.manual_seed(2)
+    eager, captured = ([DPLinear(64, 96, C=1.0, sigma=0.5, seed=3, layer=k, device=DEV, auto_step=False) for k in range(3)] for _ in range(2))
+    for a, b in zip(eager, captured):
+        a.load_state_dict(b.state_dict())
+    x, dy = torch.empty(3, T, 64, device=DEV, dtype=torch.bfloat16), torch.empty(3, T, 96, device=DEV, dtype=torch.bfloat16)
+
+    def step(ms):
+        for m in ms:
+            m.weight.grad = None
+        with deferred_weight_grads() if deferred else nullcontext():
+            for m in ms:
+                m(x).backward(dy)
+        return [m.weight.grad for m in ms]
+
+    def draw(seed):
+        torch.manual_seed(seed)
+        x.normal_()
+        dy.normal_()
+
+    draw(1)
+    step(eager)
+    torch.cuda.synchronize()
+    F.flashdp_release()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(captured)
+    for rep in range(3):
+        draw(rep)
+        want = [t.clone() for t in step(eager)]
+        big = 256 << rep
+        a, o = torch.ones(2, 64, big, device=DEV, dtype=torch.bfloat16), torch.empty(big, big, device=DEV)
+        F.flashdp_block_dp_grad([dict(X=a, dY=a, d_in=big, d_out=big, C=1.0, sigma=0.0, seed=0, layer=0, out_grad=o)], 2, 64, F.BF16, "scratch")
+        if rep == 2:
+            F.flashdp_release()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert float((g.float() - w.float()).norm() / w.float().norm()) <= 2.0 ** -8, rep      # (one step of bfloat16 where the order of additions differs)
