@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "clip_factor.hip.h"
 #include "philox_gauss.h"
 #include "vector_io.hip.h"
@@ -76,15 +78,19 @@ __global__ __launch_bounds__(256) void vector_factors_kernel(const VectorArgs a)
 }
 
 // out for COLS elements per workgroup: COLS threads of it side by side, the samples dealt to 256 / COLS rows of threads and their sums
-// joined in a fixed order.  FOLD: every workgroup works the clip factors out for itself, all samples at a time (256 / B lanes each;
+// joined in a fixed order.  COLS = 64, for at most 16 samples: a thread adds up four.  COLS = 16:
+// up to 2^16, one after the other, and so in fp64 (in fp32, 2^14 equal ones lost eleven bits).  FOLD: every workgroup works the clip factors out for itself, all samples at a time (256 / B lanes each;
 // a wave for one sample after the other takes a microsecond each: 256 samples of 512 elements 40 us, 3 so).
 constexpr int VECTOR_FOLD_B = 1024;             // factors kept in LDS
 constexpr int64_t VECTOR_FOLD_SQUARES = 8192;   // B * blocks doubles that every workgroup reads: 64 KB from the caches
+__device__ __forceinline__ float fma_of(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ double fma_of(double a, double b, double c) { return fma(a, b, c); }
 template <bool FOLD, int COLS>
 __global__ __launch_bounds__(256) void vector_clip_kernel(const VectorArgs a) {
   constexpr int ROWS = 256 / COLS, EARLY = 4;
+  using Sum = std::conditional_t<COLS == 64, float, double>;
   __shared__ float fac[FOLD ? VECTOR_FOLD_B : 1];
-  __shared__ float part[ROWS][COLS];
+  __shared__ Sum part[ROWS][COLS];
   const int c = threadIdx.x % COLS, r = threadIdx.x / COLS;
   const int64_t col = (int64_t)blockIdx.x * COLS + c;
   // what does not depend on the factors goes first: the first samples' elements, the old output, the noise
@@ -113,23 +119,23 @@ __global__ __launch_bounds__(256) void vector_clip_kernel(const VectorArgs a) {
     }
     __syncthreads();
   }
-  float s = 0.0f;
+  Sum s = 0;
   if (col < a.n) {
 #pragma unroll
     for (int k = 0; k < EARLY; ++k)
-      if (r + k * ROWS < a.B) s = fmaf(FOLD ? fac[r + k * ROWS] : a.factors[r + k * ROWS], early[k], s);
+      if (r + k * ROWS < a.B) s = fma_of((Sum)(FOLD ? fac[r + k * ROWS] : a.factors[r + k * ROWS]), (Sum)early[k], s);
 #pragma unroll 8
-    for (int64_t i = r + EARLY * ROWS; i < a.B; i += ROWS) s = fmaf(FOLD ? fac[i] : a.factors[i], a.g[i * a.n + col], s);
+    for (int64_t i = r + EARLY * ROWS; i < a.B; i += ROWS) s = fma_of((Sum)(FOLD ? fac[i] : a.factors[i]), (Sum)a.g[i * a.n + col], s);
   }
   part[r][c] = s;
   __syncthreads();
   if (r != 0 || col >= a.n) return;
-  s = 0.0f;
+  s = 0;
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) s += part[k][c];
-  if (a.accumulate) s += old;
-  if (a.noise_scale != 0.0f) s = fmaf(a.noise_scale, noise, s);
-  a.out[col] = s;
+  if (a.accumulate) s += (Sum)old;
+  if (a.noise_scale != 0.0f) s = fma_of((Sum)a.noise_scale, (Sum)noise, s);
+  a.out[col] = (float)s;
 }
 
 }  // namespace flashdp

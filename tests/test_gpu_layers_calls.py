@@ -125,3 +125,17 @@ def test_captured_layers_without_an_epilogue_outlive_the_librarys_workspace(defe
         torch.cuda.synchronize()
         for g, w in zip(got, want):
             assert float((g.float() - w.float()).norm() / w.float().norm()) <= 2.0 ** -8, rep      # (one step of bfloat16 where the order of additions differs)
+
+
+@pytest.mark.parametrize("B", [300, 5000, 1 << 18])
+@pytest.mark.parametrize("n", [1, 40])
+def test_sums_over_many_equal_samples_keep_their_bits(B, n):
+    """Nothing clips, so the factors are 1 and the sum is B times a number whose roundings on the way all point one way.  Added up in 64 bits and
+    rounded once: off by half a step of fp32, 2^-24, and less than another for the 64 bits."""
+    g = torch.full((B, 1, n), 1.0 / 3.0, device=DEV) * torch.linspace(1, 2, n, device=DEV)
+    out = torch.empty(n, device=DEV)
+    F.flashdp_activation_dp_grad(g, None, False, B, 1, n, F.F32, None, 1e6, 0.0, 0, 0, None, out)
+    want = B * g[0, 0].cpu().double()
+    assert bool(((out.cpu().double() - want).abs() <= 1.01 * 2.0 ** -24 * want).all()), float(((out.cpu().double() - want).abs() / want).max() * 2 ** 24)
+    F.flashdp_activation_dp_grad(g, None, False, B, 1, n, F.F32, None, 1e6, 0.0, 0, 0, None, out, accumulate=True)
+    assert bool(((out.cpu().double() - 2 * want).abs() <= 2.02 * 2.0 ** -24 * 2 * want).all())
