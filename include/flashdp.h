@@ -259,7 +259,8 @@ enum { FLASHDP_ACT_NONE = 0, FLASHDP_ACT_RELU = 1, FLASHDP_ACT_GELU = 2, FLASHDP
  * flashdp_checkpoint8_bytes(rows, d_out) bytes made from the fp32 sums (z_8bit = 1).  The activation is taken of the fp32 sum,
  * not of the kept Z.  Y may be residual; it may overlap nothing else.  Rows are independent of each other to the bit only among calls
  * of the same number of rows (the order of additions goes by the sizes).  fp32 products of d_in >= 64 may be formed from operands cut into three
- * bfloat16 parts (error below that of the fp32 sums), where an operand that is infinite counts as NaN.  No workspace. */
+ * bfloat16 parts: a product is then off by up to 2^-22 of itself, a sum by less than what d_in fp32 additions one after the other may be
+ * off by, and an operand that is infinite counts as NaN.  No workspace. */
 int flashdp_linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t rows, int64_t d_in, int64_t d_out,
                            int dtype, int activation, void* Y, void* Z, int z_8bit, void* stream);
 

@@ -205,12 +205,11 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
 // bf16 1 x 4096 -> 4096: 7.2, 10.0, 10.0, 14.7, 34, -, -; fp16 8 x 768 -> 50257: 23.3, 16.6, 18.4, 22.4, -, -, -; bf16 128 x 4096 -> 4096: -, -, 14.6, 15.2, 34.9, 46, 74;
 // 256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
 // bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; 8192 x 768 -> 3072: -, -, 167, 109, 62, 51, 51, with GELU and Z in 8 bits -, -, -, 127, 80, 62, 69.
-// fp32, 32 x 32, 64 x 64, 128 x 128 twice, then in bfloat16 parts on 64 x 128 and 128 x 256: 128 x 4096 -> 4096: 48, 74, 247, 127, 267; 512 x 4096 -> 4096: 169,
-// 148, 249, 142, 273; 2048 x 4096 -> 4096: 663, 586, 478, 385, 303; 8192 x 768 -> 3072: 429, 382, 286, 228, 194.  Relative errors in norm there, fp32
-// instruction and parts: 1.15e-6, 1.02e-6; K = 768: 5.0e-7, 4.4e-7.
+// fp32, 32 x 32, 64 x 64, 128 x 128 twice, then in bfloat16 parts on 64 x 128 and 128 x 256: 128 x 4096 -> 4096: 55, 78, 247, 153, 287; 512 x 4096 -> 4096: 173,
+// 150, 249, 138, 292; 2048 x 4096 -> 4096: 663, 586, 478, 400, 318; 8192 x 768 -> 3072: 429, 382, 286, 239, 198 (errors: forward_split.hip.h).
 // Rows that no 16-byte chunks divide: direct loads to LDS need 4-byte alignment; few rows take the kernel that reads W straight into
 // registers, others tiles staged through registers (bf16 64 x 4096 -> 4096: 23.8, 39.5), fp32 the parts where they are faster
-// (1024 x 1001 -> 2304: 71, 57).
+// (1024 x 1001 -> 2304: 70, 59).
 enum ForwardPath { FWD_16x16 = 0, FWD_16x32, FWD_32x32, FWD_64x64, FWD_128x128, FWD_128x128_TWO, FWD_256x256, FWD_ROWS, FWD_ANY_64, FWD_ANY_128, FWD_SPLIT, FWD_SPLIT_SMALL, FWD_PATHS };
 struct ForwardCost { double start, tile, alone; };
 struct ForwardRung { ForwardPath path; int bm, bn, per_cu; ForwardCost bits16, bits32; double epilogue; bool direct; };   // no tile: not for that type
@@ -218,9 +217,9 @@ constexpr ForwardRung FORWARD_LADDER[] = {
     {FWD_16x16, 16, 16, 2, {1.9, 0.115, 0.085}, {1.9, 0.115, 0.09}, 0.2, true},   {FWD_16x32, 16, 32, 3, {2.0, 0.15, 0.12}, {2.0, 0.3, 0.21}, 0.3, true},
     {FWD_32x32, 32, 32, 2, {1.6, 0.18, 0.1}, {1.6, 0.34, 0.2}, 0.4, true},        {FWD_64x64, 64, 64, 1, {2.6, 0.19, 0.19}, {2.6, 0.56, 0.56}, 0.7, true},
     {FWD_128x128, 128, 128, 1, {4.0, 0.54, 0.54}, {}, 2.9, true},                 {FWD_128x128_TWO, 128, 128, 2, {6.6, 0.87, 0.65}, {6.6, 3.7, 1.92}, 3.7, true},
-    {FWD_256x256, 256, 256, 1, {7.0, 1.54, 1.54}, {}, 9.0, true},                 {FWD_SPLIT, 128, 256, 1, {}, {9.5, 2.32, 2.02}, 4.5, false},
-    {FWD_SPLIT_SMALL, 64, 128, 2, {}, {5.6, 1.45, 0.95}, 2.0, false}};
-constexpr int64_t SPLIT_LEAST = 64;   // fewest products of a sum formed from parts: their error is allowed from there on (forward_split.hip.h)
+    {FWD_256x256, 256, 256, 1, {7.0, 1.54, 1.54}, {}, 9.0, true},                 {FWD_SPLIT, 128, 256, 1, {}, {9.5, 2.43, 2.2}, 4.5, false},
+    {FWD_SPLIT_SMALL, 64, 128, 2, {}, {5.6, 1.53, 0.98}, 2.0, false}};
+constexpr int64_t SPLIT_LEAST = 64;   // fewest products of a sum formed from parts: from there on they are closer than the fp32 instruction in every way (forward_split.hip.h)
 
 bool forward_direct(int64_t d_in, int dtype) { return d_in * (dtype == FLASHDP_F32 ? 4 : 2) % 16 == 0; }
 // 256 rows lie within the 2 GiB that a buffer descriptor reaches

@@ -139,3 +139,35 @@ def test_sums_over_many_equal_samples_keep_their_bits(B, n):
     assert bool(((out.cpu().double() - want).abs() <= 1.01 * 2.0 ** -24 * want).all()), float(((out.cpu().double() - want).abs() / want).max() * 2 ** 24)
     F.flashdp_activation_dp_grad(g, None, False, B, 1, n, F.F32, None, 1e6, 0.0, 0, 0, None, out, accumulate=True)
     assert bool(((out.cpu().double() - 2 * want).abs() <= 2.02 * 2.0 ** -24 * 2 * want).all())
+
+
+@pytest.mark.parametrize("kernel", [None, 10, 11])
+@pytest.mark.parametrize("K", [64, 128, 773, 4096])
+@pytest.mark.parametrize("kind", ["just above one", "one product", "rectified", "normal"])
+def test_single_precision_products_keep_single_precision(kind, K, kernel):
+    """fp32 operands in bfloat16 parts, where they are taken.  u = 2^-24.  A product of two floats: the parts left out are below 2^-22 of it, 4 u.  A k-tile of 32
+    products: six matrix instructions, of which the last, with the largest parts, cuts its sum off within a step, 2 u, and the ones before it, of
+    parts below 2^-7, less than that together.  Then K / 32 additions that round by u each.  Products of one sign show whether what is cut off adds up."""
+    rows, D = 200, 264
+    g = torch.Generator().manual_seed(K)
+    if kind == "just above one":
+        x, w = (1 + torch.rand(n, K, generator=g) * 2.0 ** -6 for n in (rows, D))
+    elif kind == "one product":
+        x, w = torch.zeros(rows, K), 1 + torch.rand(D, K, generator=g)
+        x[torch.arange(rows), torch.randint(K, (rows,), generator=g)] = 1 + torch.rand(rows, generator=g)
+        x[0, x[0] != 0] = 1 + 2.0 ** -7 - 2.0 ** -23
+        w[0] = 1 + 2.0 ** -7 - 2.0 ** -23
+    elif kind == "rectified":
+        x, w = torch.randn(rows, K, generator=g).clamp(min=0), torch.rand(D, K, generator=g)
+    else:
+        x, w = torch.randn(rows, K, generator=g), torch.randn(D, K, generator=g)
+    y = torch.empty(rows, D, device=DEV)
+    with env(FLASHDP_FORWARD=kernel):
+        F.flashdp_linear_forward(x.to(DEV), w.to(DEV), None, None, rows, K, D, F.F32, None, y)
+        assert kernel is None or F.flashdp_last_kernel() == "forward_split_kernel"
+    x64, w64 = x.double(), w.double()
+    want, size = x64 @ w64.T, x64.abs() @ w64.abs().T
+    u = 2.0 ** -24
+    # (the fp32 instructions, where the parts are not taken, add K products in a row)
+    steps = 4 + 2 + 2 + (K + 31) // 32 if kernel is not None else K + 2
+    assert bool(((y.cpu().double() - want).abs() <= steps * u * size).all()), float(((y.cpu().double() - want).abs() / size).max() / u)
