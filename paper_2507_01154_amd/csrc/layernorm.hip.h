@@ -215,9 +215,12 @@ __global__ __launch_bounds__(THREADS) void layernorm_grad_kernel(const NormGradA
       widen_chunk<DT>(xr[c], f);
       widen_chunk<DT>(gr[c], e);
       widen_chunk<DT>(w[c], v);
+      // (columns and rows that do not exist have dy = 0, and need xh = 0 as well: the mean alone times rstd may be infinite)
+      const int64_t left = a.d - (int64_t)(c * NT + t) * N;
+      const float here = EVEN && left <= 0 ? 0.0f : mu;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {     // (columns and rows that do not exist have dy = 0)
-        const float xh = (f[k] - mu) * r, p = e[k] * v[k];
+      for (int k = 0; k < N; ++k) {
+        const float xh = EVEN || k < left ? (f[k] - here) * r : 0.0f, p = e[k] * v[k];
         s[0] += p;
         s[1] = fmaf(p, xh, s[1]);
         sg[c][k] = fmaf(e[k], xh, sg[c][k]);
@@ -352,7 +355,7 @@ __global__ __launch_bounds__(256) void layernorm_grad_long_rows_kernel(const Nor
     for (int k = 0; k < N; ++k) {
       const float p = g[k] * v[k];
       s[0] += p;
-      s[1] = fmaf(p, (f[k] - mu) * r, s[1]);
+      s[1] = fmaf(p, k < a.d - col ? (f[k] - mu) * r : 0.0f, s[1]);
     }
   }
   group_sum(s, lds);

@@ -171,3 +171,25 @@ def test_single_precision_products_keep_single_precision(kind, K, kernel):
     # (the fp32 instructions, where the parts are not taken, add K products in a row)
     steps = 4 + 2 + 2 + (K + 31) // 32 if kernel is not None else K + 2
     assert bool(((y.cpu().double() - want).abs() <= steps * u * size).all()), float(((y.cpu().double() - want).abs() / size).max() / u)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [1, 6])
+@pytest.mark.parametrize("d", [72, 75, 1032, 1035, 8200, 16408, 20001])
+def test_a_mean_whose_product_with_rstd_overflows(d, T, dtype):
+    """Constant rows: x - mean is zero, and so is every normalised value, but mean * rstd is not finite: what lies between a row's end and the last
+    thread's must not enter its sums as zero times infinity.  dx = rstd (a - mean(a)): d / 64 + 10 additions of fp32 and one rounding to the type."""
+    B, c, r = 2, 2.0 ** 121, 2.0 ** 8
+    torch.manual_seed(d)
+    x, dy = torch.full((B * T, d), c, device=DEV, dtype=dtype), torch.randn(B, T, d, device=DEV).to(dtype)
+    gam = torch.randn(d, device=DEV).to(dtype)
+    mean, rstd = torch.full((B * T,), c, device=DEV), torch.full((B * T,), r, device=DEV)
+    dx, g, n = torch.empty_like(dy), torch.empty(2, d, device=DEV), torch.empty(B, device=DEV)
+    F.flashdp_layernorm_dp_grad(x, dy, gam, mean, rstd, B, T, d, F.dtype_code(x), 1e6, 0.0, 0, 0, dx, g, n)
+    dy64, a = dy.cpu().double(), dy.cpu().double() * gam.cpu().double()
+    want = r * (a - a.mean(-1, keepdim=True))
+    slack = r * ((d / 64 + 10) * 2.0 ** -24 * a.abs().mean(-1, keepdim=True) + 2.0 ** -22 * a.abs())
+    assert bool(((dx.cpu().double() - want).abs() <= 1.01 * slack + torch.finfo(dtype).eps / 2 * want.abs()).all())
+    total = dy64.sum(1)
+    assert bool((g[0] == 0).all()) and bool(((g[1].cpu().double() - total.sum(0)).abs() <= (B * T + 4) * 2.0 ** -24 * dy64.abs().sum((0, 1))).all())
+    assert bool(((n.cpu().double() - total.norm(dim=1)).abs() <= (T + 4) * 2.0 ** -24 * dy64.abs().sum(1).norm(dim=1)).all())
