@@ -193,3 +193,44 @@ def test_a_mean_whose_product_with_rstd_overflows(d, T, dtype):
     total = dy64.sum(1)
     assert bool((g[0] == 0).all()) and bool(((g[1].cpu().double() - total.sum(0)).abs() <= (B * T + 4) * 2.0 ** -24 * dy64.abs().sum((0, 1))).all())
     assert bool(((n.cpu().double() - total.norm(dim=1)).abs() <= (T + 4) * 2.0 ** -24 * dy64.abs().sum(1).norm(dim=1)).all())
+
+
+# rows of 2048 elements on both sides of 2^30 and 2^31 elements, the ends of both samples, and some others; each with a power of two of its own
+MARKED = [0, 1, 255, 256, 4095, 99999, 524287, 524288, 549999, 550000, 550001, 786432, 1000003, 1048575, 1048576, 1048577, 1099990, 1099999]
+
+
+def marked_gradient(B, rows, d):
+    """dY that is zero but for the marked rows, and its sum over each sample's tokens: every row read once or the sum is another number, exactly."""
+    dy, per = torch.zeros(rows, d, device=DEV, dtype=torch.bfloat16), 1.0 + torch.arange(d, device=DEV) % 3
+    sums = torch.zeros(B, d, dtype=torch.float64, device=DEV)
+    for k, r in enumerate(MARKED):
+        dy[r] = (2.0 ** k * per).bfloat16()
+        sums[r * B // rows] += 2.0 ** k * per.double()
+    return dy, sums
+
+
+def test_every_row_of_long_inputs_enters_the_gradients_of_vectors_once():
+    """1100000 x 2048: bias (ReLU of ones, Z as it is and in 8 bits) and layer norm (mean 0, rstd 1, x of -2 .. 2).  All sums are whole numbers below 2^24."""
+    B, rows, d = 2, 1100000, 2048
+    T = rows // B
+    dy, sums = marked_gradient(B, rows, d)
+    z = torch.ones(rows, d, device=DEV, dtype=torch.bfloat16)
+    z8 = torch.empty(F.flashdp_checkpoint8_bytes(rows, d), dtype=torch.uint8, device=DEV)
+    F.flashdp_checkpoint8_pack(z, rows, d, F.BF16, z8)
+    g, n = torch.empty(d, device=DEV), torch.empty(B, device=DEV)
+    for kept, eight in ((z, False), (z8, True)):
+        F.flashdp_activation_dp_grad(dy, kept, eight, B, T, d, F.BF16, "relu", 1e30, 0.0, 0, 0, None, g, n)
+        assert torch.equal(g.double(), sums.sum(0))
+        assert bool(((n.double() - sums.norm(dim=1)).abs() <= 2.0 ** -24 * sums.norm(dim=1)).all())
+    del z8
+    x = z
+    x.copy_(((torch.arange(rows, device=DEV)[:, None] * 7 + torch.arange(d, device=DEV) * 3) % 5 - 2).to(torch.bfloat16))
+    want = torch.zeros(B, 2, d, dtype=torch.float64, device=DEV)
+    for r in MARKED:
+        want[r * B // rows, 0] += dy[r].double() * x[r].double()
+    want[:, 1] = sums
+    gn, mean, rstd = torch.empty(2, d, device=DEV), torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV)
+    F.flashdp_layernorm_dp_grad(x, dy, torch.ones(d, device=DEV, dtype=torch.bfloat16), mean, rstd, B, T, d, F.BF16, 1e30, 0.0, 0, 0, None, gn, n)
+    assert torch.equal(gn.double(), want.sum(0))
+    norms = want.reshape(B, -1).norm(dim=1)
+    assert bool(((n.double() - norms).abs() <= 2.0 ** -24 * norms).all())
