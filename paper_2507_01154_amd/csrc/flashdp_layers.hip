@@ -207,9 +207,12 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
 // bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; 8192 x 768 -> 3072: -, -, 167, 109, 62, 51, 51, with GELU and Z in 8 bits -, -, -, 127, 80, 62, 69.
 // fp32, 32 x 32, 64 x 64, 128 x 128 twice, then in bfloat16 parts on 64 x 128 and 128 x 256: 128 x 4096 -> 4096: 55, 78, 247, 153, 287; 512 x 4096 -> 4096: 173,
 // 150, 249, 138, 292; 2048 x 4096 -> 4096: 663, 586, 478, 400, 318; 8192 x 768 -> 3072: 429, 382, 286, 239, 198 (errors: forward_split.hip.h).
-// Rows that no 16-byte chunks divide: direct loads to LDS need 4-byte alignment; few rows take the kernel that reads W straight into
-// registers, others tiles staged through registers (bf16 64 x 4096 -> 4096: 23.8, 39.5), fp32 the parts where they are faster
-// (1024 x 1001 -> 2304: 70, 59).
+// Rows that no 16-byte chunks divide: direct loads to LDS need 4-byte alignment.  Up to 64 rows the kernel that reads W straight into
+// registers is the faster one until its workgroups of 32 features go in several rounds, sooner where rows start at odd multiples of two bytes; then tiles staged
+// through registers are, and fp32 in parts (costs of these fitted to 760 products of 1 to 64 rows, 33 to 13825, 40 to 50257 features; us, straight
+// from memory and tiles of 64 x 64, fp32 also parts on 64 x 128: bf16 1 x 4097 -> 4096: 28, 80; 64 x 4097 -> 4096: 76, 66; 64 x 4098 -> 4096: 34, 60;
+// 8 x 769 -> 50257: 54, 24; 8 x 2050 -> 50257: 59, 52; fp32 64 x 4097 -> 4096: 66, 114, 181; 8 x 4097 -> 50257: 227, 338, 233; 64 x 1001 -> 50257: 123, 94, 71).
+// Beyond, tiles of 64 x 64 or 128 x 128 and the parts where they are faster (fp32 1024 x 1001 -> 2304: 70, 59).
 enum ForwardPath { FWD_16x16 = 0, FWD_16x32, FWD_32x32, FWD_64x64, FWD_128x128, FWD_128x128_TWO, FWD_256x256, FWD_ROWS, FWD_ANY_64, FWD_ANY_128, FWD_SPLIT, FWD_SPLIT_SMALL, FWD_PATHS };
 struct ForwardCost { double start, tile, alone; };
 struct ForwardRung { ForwardPath path; int bm, bn, per_cu; ForwardCost bits16, bits32; double epilogue; bool direct; };   // no tile: not for that type
@@ -234,7 +237,6 @@ int64_t forward_tiles(int64_t rows, int64_t d_out, int bm, int bn) {
 ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, bool blocks_of_32, bool busy) {
   const int forced = api::forward_override();
   const bool f32 = dtype == FLASHDP_F32, described = forward_described(d_in, dtype), direct = described && forward_direct(d_in, dtype);
-  if (!direct && rows <= 64 && (forced < FWD_ANY_64 || forced >= FWD_PATHS)) return FWD_ROWS;
   const int64_t cus = api::compute_units(), nk = (d_in * (f32 ? 4 : 2) + 127) / 128;
   ForwardPath best = FWD_PATHS;
   double least = 0.0;
@@ -245,14 +247,20 @@ ForwardPath forward_path(int64_t rows, int64_t d_in, int64_t d_out, int dtype, b
     if (forced == path) t = -1.0;
     if (best == FWD_PATHS || t < least) { best = path; least = t; }
   };
+  const bool few = !direct && rows <= 64;
+  if (few) {      // k-tiles of 128 bytes
+    const double c = f32 || d_in % 2 == 0 ? 0.24 + 0.0043 * rows : 0.39 + 0.0116 * rows;
+    offer(FWD_ROWS, (d_out + 31) / 32, 1, ForwardCost{1.2, c, c}, 0.0);
+  }
   if (!direct) {
     const int64_t t64 = forward_tiles(rows, d_out, 64, 64), t128 = forward_tiles(rows, d_out, 128, 128);
-    const bool small = forced == FWD_ANY_64 || (forced != FWD_ANY_128 && t128 < 256);
-    if (small && t64 >= 0) offer(FWD_ANY_64, t64, 4, f32 ? ForwardCost{3.0, 2.2, 0.83} : ForwardCost{3.0, 1.0, 0.57}, 0.0);
+    const bool small = forced == FWD_ANY_64 || (forced != FWD_ANY_128 && (few || t128 < 256));
+    const ForwardCost c64 = few ? f32 ? ForwardCost{2.0, 2.2, 0.95} : ForwardCost{2.0, 1.4, 0.95 - 0.004 * rows} : f32 ? ForwardCost{3.0, 2.2, 0.83} : ForwardCost{3.0, 1.0, 0.57};
+    if (small && t64 >= 0) offer(FWD_ANY_64, t64, 4, c64, 0.0);
     else if (t128 >= 0) offer(FWD_ANY_128, t128, 2, f32 ? ForwardCost{6.6, 4.4, 2.2} : ForwardCost{6.6, 1.28, 0.9}, 0.0);
   }
   for (const ForwardRung& g : FORWARD_LADDER) {
-    const ForwardCost& c = f32 ? g.bits32 : g.bits16;
+    const ForwardCost c = few && f32 && g.path == FWD_SPLIT_SMALL ? ForwardCost{5.6, 1.75, 1.3} : f32 ? g.bits32 : g.bits16;
     if (c.tile == 0.0 || (g.direct ? !direct : !described || (d_in < SPLIT_LEAST && forced != g.path)) || (blocks_of_32 && g.bn % CKPT8_BLOCK != 0)) continue;
     const int64_t tiles = forward_tiles(rows, d_out, g.bm, g.bn);
     if (tiles >= 0) offer(g.path, tiles, g.per_cu, c, g.epilogue);

@@ -4,7 +4,10 @@
 // A workgroup owns 16 NF features.  Its waves share out the k-steps (64 bytes of every row) in turn, so that together they walk along
 // the rows of W in whole cache lines; every wave multiplies 16 NF features with 16 MT tokens straight from memory, up to eight k-steps' loads in
 // flight, and the waves' partial sums are joined in LDS in a fixed order.  Rows that do not exist repeat the last one that does: a sum
-// belongs to one row of each operand, and those are not kept.  bf16 64 x 4096 -> 4096: 23.8 us.
+// belongs to one row of each operand, and those are not kept.
+//
+// Bound by the loads, 16 bytes at any address: bf16 1 x 4097 -> 4096, where every other row starts at an odd multiple of two bytes, 28 us, 64 rows 76;
+// 1 x 4098 -> 4096, at multiples of four, 16 us = 2.1 TB/s of W, 64 rows 34; fp32 1 x 4097 -> 4096 28 us = 2.4 TB/s.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -234,3 +234,13 @@ def test_every_row_of_long_inputs_enters_the_gradients_of_vectors_once():
     assert torch.equal(gn.double(), want.sum(0))
     norms = want.reshape(B, -1).norm(dim=1)
     assert bool(((n.double() - norms).abs() <= 2.0 ** -24 * norms).all())
+
+
+@pytest.mark.parametrize("rows,K,D,dtype,kernel", [(1, 4097, 1000, "bf16", "forward_rows_kernel"), (64, 2049, 1000, "f16", "forward_tile_kernel"), (8, 769, 50257, "f16", "forward_tile_kernel"),
+                                                   (8, 770, 8192, "bf16", "forward_rows_kernel"), (33, 515, 50257, "fp32", "forward_split_kernel"), (16, 515, 4000, "fp32", "forward_rows_kernel"),
+                                                   (64, 33, 20001, "bf16", "forward_tile_kernel"), (64, 3001, 17001, "bf16", "forward_tile_kernel"), (2, 33, 50257, "fp32", "forward_tile_kernel")])
+def test_few_rows_that_no_chunks_divide_take_the_kernel_of_the_shorter_rounds(rows, K, D, dtype, kernel):
+    from test_gpu_layers import check_forward
+    check_forward(rows, K, D, dtype, "gelu_tanh", True, False, "8bit" if dtype != "fp32" else "dtype", seed=K)
+    check_forward(rows, K, D, dtype, "none", False, True, None, seed=D)
+    assert F.flashdp_last_kernel() == kernel
