@@ -304,7 +304,8 @@ int flashdp_checkpoint8_unpack(const void* packed, int64_t rows, int64_t d, int 
  * and results are that call's on the unpacked activation, with a null workspace or one of that much less than the caller's.  Layers of
  * different X follow each other as calls of their own, so nothing of theirs overlaps or shares a launch (and the order of additions of
  * short sequences, which are formed in groups, can differ from that of one call for all).
- * Workspace: flashdp_workspace_bytes_checkpoint8. */
+ * Workspace: flashdp_workspace_bytes_checkpoint8; with none, the activation is unpacked into memory of the library's own beside its workspace, under
+ * the same rule (calls without a workspace are ordered on one stream). */
 int flashdp_block_dp_grad_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule, void* workspace,
                                       size_t workspace_bytes, void* stream, int accumulate, int add_noise);
 size_t flashdp_workspace_bytes_checkpoint8(const flashdp_layer_t* layers, int n_layers, int64_t B, int64_t T, int dtype, int schedule);

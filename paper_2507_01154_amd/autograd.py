@@ -275,8 +275,11 @@ class DPLinear(_DPModule):
     bias: a bias whose gradient is clipped and noised by itself (threshold bias_C, by default C; norms in last_bias_norms, the fp32 sum in
     bias_grad_fp32), which makes sqrt(C^2 + bias_C^2) the layer's sensitivity.  activation: None, "relu", "gelu", "gelu_tanh" or
     "silu".  checkpoint: None keeps the input and the sum in front of the activation as they are between forward and backward pass,
-    "8bit" keeps both in 8 bits (flashdp_checkpoint8_pack), about half the memory; the gradients are those at the values that were
-    kept, clipped for what they are."""
+    "8bit" keeps both in 8 bits (flashdp_checkpoint8_pack), 33/32 bytes an element instead of 2 or 4; the gradients are those at the values that
+    were kept, clipped for what they are.  Every layer keeps a checkpoint of its own: layers that share an input (q, k, v; gate and up) share one tensor
+    without checkpoints, so three of them in 16-bit types keep 3.1 bytes an element with checkpoints and 2 without.
+
+    The weight gradient takes the library's workspace, one per device: backward passes of one device run on one stream."""
 
     def __init__(self, d_in: int, d_out: int, C: float = 1.0, sigma: float = 1.0, seed: int = 0, layer: int = 0,
                  schedule="auto", dtype=torch.bfloat16, device="cuda", auto_step: bool = True, keep_fp32_grad: bool = False,

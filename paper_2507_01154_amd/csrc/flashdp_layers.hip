@@ -201,7 +201,8 @@ NormPlan norm_plan(int64_t B, int64_t T, int64_t d, int dtype) {
 // the shortest.  A round of `per_cu` workgroups on every compute unit takes start + tile * (k-tiles of 128 bytes) microseconds, one
 // of at most one workgroup per unit start + alone * k-tiles, and epilogue more where the epilogue has an activation or 8-bit sums (fitted to 170
 // products of one to 8192 rows, 768 to 13824 features; 16-bit types, then fp32, whose k-tiles are half as deep).  us, tiles of 16 x 16, 16 x 32, 32 x 32,
-// 64 x 64, 128 x 128, 128 x 128 with two workgroups per unit, 256 x 256 (- = not tried):
+// 64 x 64, 128 x 128, 128 x 128 with two workgroups per unit, 256 x 256 (- = not tried), operands in the caches (from memory the order is the
+// same: 128 x 4096 -> 4096: -, -, 20, 21, 40, 64, 99; 512 x 4096 -> 4096: -, -, 61, 39, 40, 63, 103; 256 x 5120 -> 13824: -, -, 144, 100, 58, 89, 148):
 // bf16 1 x 4096 -> 4096: 7.2, 10.0, 10.0, 14.7, 34, -, -; fp16 8 x 768 -> 50257: 23.3, 16.6, 18.4, 22.4, -, -, -; bf16 128 x 4096 -> 4096: -, -, 14.6, 15.2, 34.9, 46, 74;
 // 256 x 4096 -> 4096: -, -, 26.2, 15.9, 35.1, 46, 76; 1024 x 4096 -> 4096: -, -, 89, 59, 38.9, 49, 76; fp16 2048 x 4096 -> 4096: -, -, 178, 120, 80, 62, 80;
 // bf16 8192 x 5120 -> 13824: -, -, 3397, 2425, 1328, 1174, 907; 8192 x 768 -> 3072: -, -, 167, 109, 62, 51, 51, with GELU and Z in 8 bits -, -, -, 127, 80, 62, 69.

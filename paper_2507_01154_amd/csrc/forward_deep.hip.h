@@ -7,7 +7,7 @@
 // 64 x 64 tile reads 8 fragments of LDS for 16 instructions, one that multiplies a quarter of it 4 for 4, and LDS is what bounds
 // small tiles.  Their partial sums are joined in LDS at the end, in a fixed order.  Swizzle and fragments as in forward_large.hip.h.
 //
-// bf16 1 x 4096 -> 4096: 7.2 us = 4.7 TB/s of W; fp16 8 x 768 -> 50257: 16.3 us = 4.7 TB/s; bf16 256 x 4096 -> 4096: 15.9 us, bound by the rate at which
+// bf16 1 x 4096 -> 4096: 7.2 us = 4.7 TB/s of W; fp16 8 x 768 -> 50257: 16.3 us = 4.7 TB/s; bf16 256 x 4096 -> 4096: 15.9 us (operands in the caches; from memory 21), bound by the rate at which
 // direct loads fill LDS (about 33 bytes a clock and compute unit).
 #pragma once
 #include <hip/hip_runtime.h>
